@@ -444,6 +444,104 @@ int nsml_decompress_accumulate_host(const void* const* payloads_host, const size
                                     int W, float* dense_host, int64_t n, int zero_first,
                                     void* device_scratch, size_t scratch_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Training in 8 bits: what runs between two exchanges.  The paper has no
+ * counterpart.  All operations share one format ("q8"): int8 codes, a row per
+ * token of an activation or per output channel of a weight, and one float32
+ * scale per row:
+ *   scale  2^e, e the smallest integer with max|x| * 2^-e <= 127, held between
+ *          -126 and 121; 0 for a row of zeros; NaN for a row that holds NaN or
+ *          Inf (its codes are 0), so that what is computed from it is NaN
+ *   code   clamp(rint(x / scale), +-127), half to even
+ * and stand for code * scale.  With power-of-two scales every such value is an
+ * exact bfloat16.  Rows of codes start on 16-byte boundaries: the base is
+ * 16-byte aligned and the row stride a multiple of 16 (nsml_q8_row_bytes is the
+ * smallest); bytes between a row's end and the next row are neither read as
+ * values nor written.  Other matrices are row-major with the row stride given
+ * in elements (>= columns) and aligned to their elements; rows on 16-byte
+ * boundaries are read and written faster.  Types: NSML_F32 or NSML_BF16.
+ * Sizes: rows and columns up to NSML_Q8_MAX_ROWS / NSML_Q8_MAX_COLS; zero rows
+ * (tokens) are allowed and leave the outputs of rows alone.  Every output is
+ * reproducible bit for bit on a device.  Nothing synchronises; all calls can be
+ * captured into a graph.
+ * ---------------------------------------------------------------------- */
+#define NSML_Q8_MAX_ROWS 2147483647LL
+#define NSML_Q8_MAX_COLS 2147483632LL
+#define NSML_Q8_MAX_NORM_COLS 32768   /* widest row of the norm */
+#define NSML_Q8_MAX_DEPTH 131071      /* longest sum of nsml_q8_matmul: 128 * 128 * 131071 < 2^31 */
+#define NSML_Q8_MATMUL_WORKSPACE_BYTES 256 /* the products' workspace holds a status word only */
+
+/* Smallest row stride, in bytes, of codes with `cols` columns (0 if out of range). */
+int64_t nsml_q8_row_bytes(int64_t cols);
+
+/* nsml_q8_pack -- stores a matrix x[rows, cols] in 8 bits (an activation that is
+ * kept for the backward pass, a weight for nsml_q8_matmul): codes and scales as
+ * above.  nsml_q8_unpack restores: out = rn(code * scale), one float32 multiply. */
+int nsml_q8_pack(const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int8_t* codes, int64_t ldq,
+                 float* scales, void* stream);
+int nsml_q8_unpack(const int8_t* codes, int64_t ldq, const float* scales, int64_t rows, int64_t cols, void* out,
+                   int64_t ldo, int dtype, void* stream);
+
+/* nsml_q8_rms_norm -- RMS norm with the residual's addition and an 8-bit output:
+ *   h     = x + residual (one float32 add, rounded to dtype; residual may be
+ *           NULL: h = x)
+ *   rstd  = 1 / sqrt(sum(h^2) / cols + eps) per row; sum, quotient and root in
+ *           float64, rounded to float32 once
+ *   y     = (h * rstd) * weight, two float32 multiplies
+ *   codes, scales = q8 of y
+ *   x, residual, h   rows x cols of dtype; h may be NULL (not written) and may
+ *                    be x or residual itself
+ *   weight           cols elements of weight_dtype
+ *   rstd             rows float32, may be NULL; the backward pass needs it
+ *   eps              > 0;  cols <= NSML_Q8_MAX_NORM_COLS */
+int nsml_q8_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t rows, int64_t cols, int dtype,
+                     const void* weight, int weight_dtype, float eps, void* h, int64_t ldh, int8_t* codes, int64_t ldq,
+                     float* scales, float* rstd, void* stream);
+
+/* nsml_q8_rms_norm_backward -- its gradient (rounding to codes counts as the
+ * identity):  n = h * rstd, g = dy * weight, c = sum(g * n) / cols,
+ *   dx      = rstd * (g - n * c) [+ dh]       (also the residual's gradient)
+ *   dweight = [dweight +] sum over rows of dy * n
+ * in float32, each output rounded once.
+ *   h              the rows that were normalised, as nsml_q8_rms_norm left them,
+ *                  or NULL and codes + scales: their checkpoint by nsml_q8_pack
+ *   dh             NULL, or a gradient that reaches h past the norm
+ *   dx             may be dy or dh itself
+ *   dweight        cols elements of dweight_dtype (aligned to its elements: a
+ *                  slice of a gradient bucket), or NULL; zero_first = 0 adds
+ *   workspace      256-byte aligned, nsml_q8_rms_norm_backward_workspace_bytes(cols)
+ *                  bytes; not needed (may be NULL) without dweight */
+size_t nsml_q8_rms_norm_backward_workspace_bytes(int64_t cols);
+int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64_t lddh, const void* h, int64_t ldh,
+                              const int8_t* codes, int64_t ldq, const float* scales, const float* rstd, int64_t rows,
+                              int64_t cols, int dtype, const void* weight, int weight_dtype, void* dx, int64_t lddx,
+                              void* dweight, int dweight_dtype, int zero_first, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/* nsml_q8_matmul -- product of activations a[m, k] and weights b[n, k], both q8:
+ *   out[i, j] = (sum_t a[i, t] * b[j, t]) * a_scales[i] * b_scales[j]
+ * The sum is exact (32-bit integers; k <= NSML_Q8_MAX_DEPTH), then two float32
+ * multiplies and one rounding to dtype.  Any int8 codes and float32 scales. */
+int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const int8_t* b, int64_t ldb, const float* b_scales,
+                   int64_t m, int64_t n, int64_t k, void* out, int64_t ldo, int dtype, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/* Its gradients, from dy[m, n] (bfloat16, 16-byte aligned, row stride a multiple
+ * of 8 elements) and what the forward pass kept:
+ *   nsml_q8_matmul_grad_input    dx[m, k] = sum_j dy[i, j] * (b[j, t] * b_scales[j])
+ *   nsml_q8_matmul_grad_weight   dw[n, k] = [dw +] sum_i dy[i, j] * (a[i, t] * a_scales[i])
+ * code * scale enters the product as a bfloat16: exact for power-of-two scales
+ * from 2^-126 to 2^119, rounded to nearest otherwise.  Sums are float32, each
+ * output is rounded once (zero_first = 0: after one float32 add).  dw may be a
+ * slice of a gradient bucket (aligned to its elements, any row stride >= k).
+ * m = 0 leaves a sum of nothing: dw is zeroed, or left as it is. */
+int nsml_q8_matmul_grad_input(const void* dy, int64_t ldy, const int8_t* b, int64_t ldb, const float* b_scales, int64_t m,
+                              int64_t n, int64_t k, void* dx, int64_t lddx, int dtype, void* workspace,
+                              size_t workspace_bytes, void* stream);
+int nsml_q8_matmul_grad_weight(const void* dy, int64_t ldy, const int8_t* a, int64_t lda, const float* a_scales, int64_t m,
+                               int64_t n, int64_t k, void* dw, int64_t lddw, int dtype, int zero_first, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream`, then copies the status word of `workspace` (or of a
  * host-variant `device_scratch`) to *status_out (host pointer): NSML_OK or the
  * first device-detected error of the last call that used it. */

@@ -117,6 +117,16 @@ def _load() -> ctypes.CDLL:
         "nsml_adaptive_workspace_bytes": (sz, [i64, ci]),
         "nsml_compress_adaptive": (ci, [vp, i64, ci, dbl, dbl, dbl, ci, vp, vp, vp, sz, vp, sz, vp,
                                         ctypes.POINTER(dbl), ctypes.POINTER(ci), ctypes.POINTER(dbl)]),
+        "nsml_q8_row_bytes": (i64, [i64]),
+        "nsml_q8_pack": (ci, [vp, i64, i64, i64, ci, vp, i64, vp, vp]),
+        "nsml_q8_unpack": (ci, [vp, i64, vp, i64, i64, vp, i64, ci, vp]),
+        "nsml_q8_rms_norm": (ci, [vp, i64, vp, i64, i64, i64, ci, vp, ci, ctypes.c_float, vp, i64, vp, i64, vp, vp, vp]),
+        "nsml_q8_rms_norm_backward_workspace_bytes": (sz, [i64]),
+        "nsml_q8_rms_norm_backward": (ci, [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, ci, vp, ci, vp, i64, vp, ci,
+                                           ci, vp, sz, vp]),
+        "nsml_q8_matmul": (ci, [vp, i64, vp, vp, i64, vp, i64, i64, i64, vp, i64, ci, vp, sz, vp]),
+        "nsml_q8_matmul_grad_input": (ci, [vp, i64, vp, i64, vp, i64, i64, i64, vp, i64, ci, vp, sz, vp]),
+        "nsml_q8_matmul_grad_weight": (ci, [vp, i64, vp, i64, vp, i64, i64, i64, vp, i64, ci, ci, vp, sz, vp]),
         "nsml_selftest_bounded_wait": (ci, [vp, sz, ci, vp]),
         "nsml_last_status": (ci, [vp, vp, ctypes.POINTER(ci)]),
         "nsml_strerror": (ctypes.c_char_p, [ci]),
@@ -501,6 +511,200 @@ def nsml_decompress_accumulate_host(payloads_host: Sequence, dense_host, zero_fi
                                              device_scratch.numel(), _stream_ptr(stream))
     _check(rc, "nsml_decompress_accumulate_host")
     return dense_host
+
+
+# --------------------------------------------------------------------------
+# training in 8 bits: q8 codes (int8, a row per token or output channel) and scales (float32, one per row)
+# --------------------------------------------------------------------------
+NSML_Q8_MATMUL_WORKSPACE_BYTES = 256
+
+
+def _matrix(t, what: str, rows: Optional[int] = None, cols: Optional[int] = None, dtype=None):
+    """Checks a 2-D CUDA tensor of the current device with contiguous rows; returns (pointer, row stride)."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{what} must have shape ({rows}, {cols}), not {tuple(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
+    _on_current_device(t, what)
+    return t.data_ptr(), t.stride(0)
+
+
+def _vector(t, what: str, n: int, dtype=None):
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what} must be a contiguous 1-D tensor of {n} elements")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
+    _on_current_device(t, what)
+    return t.data_ptr()
+
+
+def _on_current_device(t, what: str) -> None:
+    if not t.is_cuda or t.device.index != _torch().cuda.current_device():
+        raise ValueError(f"{what} must be a tensor of the current CUDA device")
+
+
+def _q8_dtype(dtype) -> int:
+    torch = _torch()
+    if dtype == torch.float32:
+        return NSML_F32
+    if dtype == torch.bfloat16:
+        return NSML_BF16
+    raise TypeError("matrices must be float32 or bfloat16")
+
+
+def _workspace(workspace, nbytes: int, device):
+    if workspace is None:
+        return alloc_bytes(nbytes, device)
+    _on_current_device(workspace, "workspace")
+    return workspace
+
+
+def nsml_q8_row_bytes(cols: int) -> int:
+    return int(lib.nsml_q8_row_bytes(int(cols)))
+
+
+def nsml_q8_empty(rows: int, cols: int, device):
+    """Uninitialised codes (int8 [rows, cols] whose rows start on 16-byte boundaries) and scales (float32 [rows])."""
+    torch = _torch()
+    padded = nsml_q8_row_bytes(cols)
+    if padded == 0:
+        raise NsmlError(NSML_ERR_ARG, "nsml_q8_empty")
+    return torch.empty(rows, padded, dtype=torch.int8, device=device)[:, :cols], torch.empty(rows, device=device)
+
+
+def nsml_q8_pack(x, codes=None, scales=None, stream=None):
+    """Stores x (float32 / bfloat16 [rows, cols]) in 8 bits; returns (codes, scales)."""
+    torch = _torch()
+    xp, ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    if codes is None or scales is None:
+        new = nsml_q8_empty(rows, cols, x.device)
+        codes, scales = new[0] if codes is None else codes, new[1] if scales is None else scales
+    cp, ldq = _matrix(codes, "codes", rows, cols, torch.int8)
+    sp = _vector(scales, "scales", rows, torch.float32)
+    _check(lib.nsml_q8_pack(xp, rows, cols, ldx, _q8_dtype(x.dtype), cp, ldq, sp, _stream_ptr(stream)), "nsml_q8_pack")
+    return codes, scales
+
+
+def nsml_q8_unpack(codes, scales, dtype=None, out=None, stream=None):
+    """Restores codes * scales as `dtype` (default: bfloat16), or as out's type into `out`."""
+    torch = _torch()
+    cp, ldq = _matrix(codes, "codes", dtype=torch.int8)
+    rows, cols = codes.shape
+    sp = _vector(scales, "scales", rows, torch.float32)
+    if out is None:
+        out = torch.empty(rows, cols, dtype=torch.bfloat16 if dtype is None else dtype, device=codes.device)
+    op, ldo = _matrix(out, "out", rows, cols, dtype)
+    _check(lib.nsml_q8_unpack(cp, ldq, sp, rows, cols, op, ldo, _q8_dtype(out.dtype), _stream_ptr(stream)), "nsml_q8_unpack")
+    return out
+
+
+def nsml_q8_rms_norm(x, weight, eps: float = 1e-5, residual=None, h=None, codes=None, scales=None, rstd=None, stream=None):
+    """RMS norm of x + residual with an 8-bit output: returns (codes, scales, rstd, h).
+
+    h is x + residual (a tensor of x's type, allocated unless given; x itself when there is no residual and no h given).
+    In place: h may be x or residual."""
+    torch = _torch()
+    xp, ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    wp = _vector(weight, "weight", cols)
+    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", rows, cols, x.dtype)
+    if h is None and residual is not None:
+        h = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
+    hp, ldh = (None, 0) if h is None else _matrix(h, "h", rows, cols, x.dtype)
+    if codes is None or scales is None:
+        new = nsml_q8_empty(rows, cols, x.device)
+        codes, scales = new[0] if codes is None else codes, new[1] if scales is None else scales
+    cp, ldq = _matrix(codes, "codes", rows, cols, torch.int8)
+    sp = _vector(scales, "scales", rows, torch.float32)
+    if rstd is None:
+        rstd = torch.empty(rows, device=x.device)
+    _check(lib.nsml_q8_rms_norm(xp, ldx, rp, ldr, rows, cols, _q8_dtype(x.dtype), wp, _q8_dtype(weight.dtype), float(eps), hp, ldh,
+                                cp, ldq, sp, _vector(rstd, "rstd", rows, torch.float32), _stream_ptr(stream)), "nsml_q8_rms_norm")
+    return codes, scales, rstd, x if h is None else h
+
+
+def nsml_q8_rms_norm_backward(dy, weight, rstd, h=None, codes=None, scales=None, dh=None, dx=None, dweight=None,
+                              zero_first: bool = True, workspace=None, stream=None):
+    """Gradient of nsml_q8_rms_norm: returns (dx, dweight).  The normalised rows come as h or as their checkpoint (codes and
+    scales of nsml_q8_pack(h)).  dh: a gradient that reaches h past the norm, added to dx.  dweight: float32 / bfloat16
+    tensor (a slice of a gradient bucket), float32 and allocated unless given; zero_first=False adds to it."""
+    torch = _torch()
+    dyp, ldy = _matrix(dy, "dy")
+    rows, cols = dy.shape
+    if (h is None) == (codes is None):
+        raise ValueError("give h, or codes and scales")
+    wp, rp = _vector(weight, "weight", cols), _vector(rstd, "rstd", rows, torch.float32)
+    hp, ldh = (None, 0) if h is None else _matrix(h, "h", rows, cols, dy.dtype)
+    cp, ldq = (None, 0) if codes is None else _matrix(codes, "codes", rows, cols, torch.int8)
+    sp = None if codes is None else _vector(scales, "scales", rows, torch.float32)
+    dhp, lddh = (None, 0) if dh is None else _matrix(dh, "dh", rows, cols, dy.dtype)
+    if dx is None:
+        dx = torch.empty(rows, cols, dtype=dy.dtype, device=dy.device)
+    dxp, lddx = _matrix(dx, "dx", rows, cols, dy.dtype)
+    if dweight is None:
+        dweight = torch.empty(cols, device=dy.device)
+        zero_first = True
+    dwp = _vector(dweight, "dweight", cols)
+    workspace = _workspace(workspace, int(lib.nsml_q8_rms_norm_backward_workspace_bytes(cols)), dy.device)
+    _check(lib.nsml_q8_rms_norm_backward(dyp, ldy, dhp, lddh, hp if rows else None, ldh, cp, ldq, sp, rp, rows, cols, _q8_dtype(dy.dtype), wp,
+                                         _q8_dtype(weight.dtype), dxp, lddx, dwp, _q8_dtype(dweight.dtype), 1 if zero_first else 0,
+                                         workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)), "nsml_q8_rms_norm_backward")
+    return dx, dweight
+
+
+def nsml_q8_matmul(a, a_scales, b, b_scales, out=None, dtype=None, workspace=None, stream=None):
+    """Activations a [m, k] times weights b [n, k], both q8: out [m, n] (bfloat16 unless dtype or out says float32)."""
+    torch = _torch()
+    ap, lda = _matrix(a, "a", dtype=torch.int8)
+    m, k = a.shape
+    bp, ldb = _matrix(b, "b", b.shape[0], k, torch.int8)
+    n = b.shape[0]
+    if out is None:
+        out = torch.empty(m, n, dtype=torch.bfloat16 if dtype is None else dtype, device=a.device)
+    op, ldo = _matrix(out, "out", m, n, dtype)
+    workspace = _workspace(workspace, NSML_Q8_MATMUL_WORKSPACE_BYTES, a.device)
+    _check(lib.nsml_q8_matmul(ap, lda, _vector(a_scales, "a_scales", m, torch.float32), bp, ldb, _vector(b_scales, "b_scales", n, torch.float32),
+                              m, n, k, op, ldo, _q8_dtype(out.dtype), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)), "nsml_q8_matmul")
+    return out
+
+
+def nsml_q8_matmul_grad_input(dy, b, b_scales, dx=None, dtype=None, workspace=None, stream=None):
+    """dx [m, k] = dy [m, n] (bfloat16, rows a multiple of 16 bytes apart) times the 8-bit weights b [n, k]."""
+    torch = _torch()
+    dyp, ldy = _matrix(dy, "dy", dtype=torch.bfloat16)
+    m, n = dy.shape
+    bp, ldb = _matrix(b, "b", n, b.shape[-1], torch.int8)
+    k = b.shape[1]
+    if dx is None:
+        dx = torch.empty(m, k, dtype=torch.bfloat16 if dtype is None else dtype, device=dy.device)
+    dxp, lddx = _matrix(dx, "dx", m, k, dtype)
+    workspace = _workspace(workspace, NSML_Q8_MATMUL_WORKSPACE_BYTES, dy.device)
+    _check(lib.nsml_q8_matmul_grad_input(dyp, ldy, bp, ldb, _vector(b_scales, "b_scales", n, torch.float32), m, n, k, dxp, lddx,
+                                         _q8_dtype(dx.dtype), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)),
+           "nsml_q8_matmul_grad_input")
+    return dx
+
+
+def nsml_q8_matmul_grad_weight(dy, a, a_scales, dw=None, dtype=None, zero_first: bool = True, workspace=None, stream=None):
+    """dw [n, k] = dy [m, n] (bfloat16, rows a multiple of 16 bytes apart) transposed times the 8-bit activations a [m, k].
+    dw: float32 / bfloat16, any row stride (a slice of a gradient bucket); zero_first=False adds to it."""
+    torch = _torch()
+    dyp, ldy = _matrix(dy, "dy", dtype=torch.bfloat16)
+    m, n = dy.shape
+    ap, lda = _matrix(a, "a", m, a.shape[-1], torch.int8)
+    k = a.shape[1]
+    if dw is None:
+        dw = torch.empty(n, k, dtype=torch.float32 if dtype is None else dtype, device=dy.device)
+        zero_first = True
+    dwp, lddw = _matrix(dw, "dw", n, k, dtype)
+    workspace = _workspace(workspace, NSML_Q8_MATMUL_WORKSPACE_BYTES, dy.device)
+    _check(lib.nsml_q8_matmul_grad_weight(dyp, ldy, ap, lda, _vector(a_scales, "a_scales", m, torch.float32), m, n, k, dwp, lddw,
+                                          _q8_dtype(dw.dtype), 1 if zero_first else 0, workspace.data_ptr(), workspace.numel(),
+                                          _stream_ptr(stream)), "nsml_q8_matmul_grad_weight")
+    return dw
 
 
 # --------------------------------------------------------------------------

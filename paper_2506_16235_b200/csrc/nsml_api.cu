@@ -13,28 +13,17 @@
 #include "nsml_compact.cuh"
 #include "nsml_finalize.cuh"
 #include "nsml_grid.cuh"
+#include "nsml_launch.h"
 #include "nsml_list.cuh"
 #include "nsml_select.cuh"
 #include "nsml_small.cuh"
 
 namespace nsml {
 
-// A CUDA call failed: what the call returns.  The runtime keeps the error of a refused launch or copy for the thread's next
-// cudaGetLastError, which is not to meet it again: the calls that follow have nothing to do with it.  (Every launch is
-// checked by its own return code.)
-static int cuda_error() {
-  cudaGetLastError();
-  return NSML_ERR_CUDA;
-}
-
-enum KernelId {
-  K_SAMPLE = 0, K_COMPACT_BUCKET, K_EMIT, K_PARTITION, K_MERGE, K_CLEAR, K_SELECT_GRID,
-  K_SUMSQ, K_PRUNE_PASS, K_PRUNE_FINISH, K_SELECT_SMALL, K_COUNT
-};
-
 static const char* const kKernelNames[K_COUNT] = {"k_sample", "k_compact_bucket", "k_emit", "k_partition", "k_merge",
                                                   "k_clear", "k_select_grid", "k_sumsq", "k_prune_pass", "k_prune_finish",
-                                                  "k_select_small"};
+                                                  "k_select_small", "k_q8_pack", "k_q8_unpack", "k_q8_norm", "k_q8_norm_grad",
+                                                  "k_q8_norm_weight", "k_q8_gemm", "k_q8_tokens"};
 
 static std::atomic<int64_t> g_launches{0};
 
@@ -62,27 +51,22 @@ static void prof_drain_locked() {
   g_prof_records.clear();
 }
 
-struct LaunchScope {  // brackets one kernel launch
-  int id;
-  cudaStream_t stream;
-  cudaEvent_t start = nullptr, stop = nullptr;
-  // timed = false: never bracket this launch with events (creating events allocates)
-  LaunchScope(int id_, cudaStream_t s, bool timed = true) : id(id_), stream(s) {
-    if (timed && g_prof_on.load(std::memory_order_relaxed)) {
-      cudaEventCreate(&start);
-      cudaEventCreate(&stop);
-      cudaEventRecord(start, stream);
-    }
+LaunchScope::LaunchScope(int id_, cudaStream_t s, bool timed) : id(id_), stream(s) {
+  if (timed && g_prof_on.load(std::memory_order_relaxed)) {
+    cudaEventCreate(&start);
+    cudaEventCreate(&stop);
+    cudaEventRecord(start, stream);
   }
-  ~LaunchScope() {
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    if (start) {
-      cudaEventRecord(stop, stream);
-      std::lock_guard<std::mutex> lock(g_prof_mutex);
-      g_prof_records.push_back({id, start, stop});
-    }
+}
+
+LaunchScope::~LaunchScope() {
+  g_launches.fetch_add(1, std::memory_order_relaxed);
+  if (start) {
+    cudaEventRecord(stop, stream);
+    std::lock_guard<std::mutex> lock(g_prof_mutex);
+    g_prof_records.push_back({id, start, stop});
   }
-};
+}
 
 template <int DTYPE>
 static GridKernel<DTYPE> grid_kernel(bool feedback, bool masked, bool large) {
@@ -155,7 +139,6 @@ static int device_info(const DeviceInfo** out) {
 }
 
 static inline bool valid_bits(int bits) { return bits == NSML_BITS_INT8 || bits == NSML_BITS_FP16 || bits == NSML_BITS_FP32; }
-static inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 static inline unsigned int grid_for(unsigned long long work_items, unsigned long long per_block, int cap) {
   unsigned long long blocks = (work_items + per_block - 1) / per_block;
@@ -171,48 +154,12 @@ static inline unsigned int grid_for(unsigned long long work_items, unsigned long
 // and the list stages afterwards with nothing to overlap them (measured with a timer in every kernel, before the list
 // stage was rebuilt: 250 us of an 800 us step).  At high priority its few blocks are placed as soon as blocks of the running pass
 // retire, and it runs beside the next pass.
-static int high_priority() {
+int high_priority() {
   static const int p = [] {
     int least = 0, greatest = 0;
     return cudaDeviceGetStreamPriorityRange(&least, &greatest) == cudaSuccess ? greatest : 0;
   }();
   return p;
-}
-
-template <class... KArgs, class... Args>
-static cudaError_t launch_prio(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool cooperative,
-                               unsigned int cluster_x, bool high, bool dependent, Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[4];
-  unsigned int na = 0;
-  attr[na].id = cudaLaunchAttributePriority;
-  attr[na].val.priority = high ? high_priority() : 0;
-  ++na;
-  if (cooperative) {
-    attr[na].id = cudaLaunchAttributeCooperative;
-    attr[na].val.cooperative = 1;
-    ++na;
-  }
-  if (cluster_x) {
-    attr[na].id = cudaLaunchAttributeClusterDimension;
-    attr[na].val.clusterDim.x = cluster_x;
-    attr[na].val.clusterDim.y = 1;
-    attr[na].val.clusterDim.z = 1;
-    ++na;
-  }
-  if (dependent) {  // may start while its predecessor in the stream still runs (programmatic dependent launch); the
-                    // kernel calls pdl_wait before it touches anything the predecessor writes
-    attr[na].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[na].val.programmaticStreamSerializationAllowed = 1;
-    ++na;
-  }
-  cfg.attrs = attr;
-  cfg.numAttrs = na;
-  return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
 
 // without any attribute: at the priority of the stream
