@@ -7,9 +7,19 @@
 // In the gradients the codes' scale belongs to the axis of the sum, so it cannot wait for the epilogue: eight warps restore
 // the codes to bfloat16 on their way from one shared-memory ring to another (exact for the scales that nsml_q8_pack makes).
 // The restored matrix never exists in memory.
+//
+// Two forms.  PAIR: two blocks on neighbouring SMs share a 256 x 256 tile (cta_group::2): each loads, and restores, one half
+// of both operands, so that shared memory is read half as often per product and every code is restored once per 256 rows of
+// the result.  Otherwise a block has a 128 x 128 tile, and the blocks of a cluster have parts of the sum each, which they
+// exchange through their shared memories (distributed shared memory, added in the order of the parts): for results that are
+// too small to fill the GPU.
+//
+// The tensor cores cut float32 sums off instead of rounding them (measured: a relative error of 3e-10 per product of a sum),
+// so float32 results are summed in pieces of kPiece products, which are added with rounding.
 #include <cuda.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "nsml_launch.h"
 #include "nsml_q8.cuh"
@@ -19,7 +29,8 @@ namespace q8 {
 
 enum { kForward = 0, kGradInput = 1, kGradWeight = 2 };
 
-constexpr int kTileM = 128;
+constexpr int kPiece = 2048;                           // products per piece of a float32 sum
+constexpr int kStepsPerPiece = kPiece / 64;
 constexpr unsigned long long kWaitNs = 2000000000ull;  // a wait gives up after two seconds
 
 // ---- PTX ---------------------------------------------------------------------------------------------------------------
@@ -68,35 +79,84 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   return bar_wait_slow(bar, parity, failed);
 }
 
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+// waits for arrivals of both blocks of a pair
+__device__ __forceinline__ bool bar_try_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
+__device__ __forceinline__ bool bar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* failed) {
+  return bar_wait(bar, parity, failed) && bar_try_cluster(bar, parity);  // (the phase is over: the second look orders memory)
+}
+__device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {  // the same place in another block of the cluster
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+// bar: an address from in_block.  What the arrival announces has been fenced already (a proxy fence, or the tensor cores'
+// own): a release over the cluster would wait for all of the thread's memory once more (8192 x 8192 x 2048: 355 against 282 us).
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <int COLS>
-__device__ __forceinline__ void tmem_alloc(uint32_t slot) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "n"(COLS) : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+// PAIR: bar may be the other block's (an address from in_block)
+template <bool PAIR>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  if constexpr (PAIR)
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
-template <int COLS>
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+__device__ __forceinline__ void tma_load_1d(uint32_t dst, const CUtensorMap* map, int x, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.1d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2}], [%3];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(bar) : "memory");
+}
+
+template <bool PAIR, int COLS>
+__device__ __forceinline__ void tmem_alloc(uint32_t slot) {
+  if constexpr (PAIR) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "n"(COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "n"(COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+}
+template <bool PAIR, int COLS>
 __device__ __forceinline__ void tmem_free(uint32_t addr) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "n"(COLS));
+  if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "n"(COLS));
+  else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "n"(COLS));
 }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-// the barrier is arrived at once all tensor work issued so far by this thread is done
+// the barrier (of both blocks) is arrived at once all tensor work issued so far by this thread is done
+template <bool PAIR>
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-template <int MODE>
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
-  if constexpr (MODE == kForward)
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
+  if constexpr (PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((uint16_t)3) : "memory");
   else
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+#define NSML_TC_MMA(GROUP, KIND)                                                                                       \
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::" GROUP ".kind::" KIND              \
+               " [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory")
+template <int MODE, bool PAIR>
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+  if constexpr (MODE == kForward && PAIR) NSML_TC_MMA("2", "i8");
+  else if constexpr (MODE == kForward) NSML_TC_MMA("1", "i8");
+  else if constexpr (PAIR) NSML_TC_MMA("2", "f16");
+  else NSML_TC_MMA("1", "f16");
+}
+#undef NSML_TC_MMA
 // 32 columns of this warp's 32 lanes
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
   asm volatile(
@@ -109,6 +169,17 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// ... and back
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+      "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr) : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 // ---- operand tiles -----------------------------------------------------------------------------------------------------
 // Shared-memory descriptors of tiles with 128-byte swizzle.
 //   sum axis along the 128 bytes of a row (kForward, the rows of dy in kGradInput): groups of 8 rows are 1024 bytes apart;
@@ -118,47 +189,62 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
 __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t leading, uint32_t stride) {
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
-template <int MODE, int BN>
+// types, axes (bits 15, 16: the other axis is the contiguous one) and shape of one multiplication
+template <int MODE, bool PAIR>
 __host__ __device__ constexpr uint32_t mma_desc() {
-  return (MODE == kForward ? (2u << 4 | 1u << 7 | 1u << 10)                                          // s32 += s8 * s8
+  return (MODE == kForward ? (2u << 4 | 1u << 7 | 1u << 10)                                                        // s32 += s8 * s8
                            : (1u << 4 | 1u << 7 | 1u << 10 | (MODE == kGradWeight ? 1u << 15 : 0u) | 1u << 16))  // f32 += bf16 * bf16
-         | (uint32_t)(BN / 8) << 17 | (uint32_t)(kTileM / 16) << 24;
+         | (PAIR ? 256u / 8 << 17 | 256u / 16 << 24 : 128u / 8 << 17 | 128u / 16 << 24);
 }
 
 struct GemmArgs {
-  int64_t rows, cols;         // of the result
-  int steps;                  // blocks of the sum: 128 codes (kForward) or 64 products
-  int64_t depth;              // length of the sum
+  int64_t rows, cols;        // of the result
+  int steps;                 // blocks of the sum: 128 codes (kForward) or 64 products
+  int piece;                 // blocks per piece of the sum
+  int64_t depth;             // length of the sum
   void* out;
   int64_t ldo;
-  bool bf16, add, pair;       // pair: rows of the result start on even elements (two of them per store)
-  const float* row_scale;     // kForward
-  const float* col_scale;     // kForward
-  const float* depth_scale;   // gradients
+  bool bf16, add, vec;       // vec: rows of the result start on 16-byte boundaries
+  const float* row_scale;    // kForward
+  const float* col_scale;    // kForward
+  int scale_shift;           // gradients: where the first scale is in the tensor map's first four
   int* status;
   int64_t tiles_m, tiles_n;
 };
 
-template <int MODE, int BN>
+// A block's share of a tile is 128 rows of the first operand and 128 of the second in both forms.
+template <int MODE, bool PAIR>
 struct Shape {
-  static constexpr int kA = kTileM * 128;                              // bytes of a stage: the first operand,
-  static constexpr int kB = MODE == kForward ? BN * 128 : BN * 64;     // codes of the second
-  static constexpr int kStage = kA + kB;
-  static constexpr int kStages = 4;
-  static constexpr int kWide = MODE == kForward ? 0 : BN * 128;        // a restored tile of the second operand
-  static constexpr int kWides = 2;
+  static constexpr int kTile = PAIR ? 256 : 128;
+  static constexpr int kStage = MODE == kForward ? 2 * 128 * 128 : 128 * 128;  // bytes of a stage: the first operand; kForward: both
+  static constexpr int kStages = 6;
+  // gradients: the second operand's codes with the scales of their rows (68 of them, so that 64 start anywhere), and restored
+  static constexpr int kCode = MODE == kForward ? 0 : 128 * 64 + 384;
+  static constexpr int kCodes = 4;
+  static constexpr int kWide = MODE == kForward ? 0 : 128 * 128;
+  static constexpr int kWides = 4;
+  static constexpr int kTurn = 2;                            // warps that restore one step's codes, taking turns:
+  static constexpr int kTurns = 8 / kTurn;
+  // every turn meets every phase of its slots of the rings (a wait tells a phase from the next one only, not from the one after)
+  static_assert(kCodes % kTurns == 0 && kWides % kTurns == 0, "");
+  static constexpr int kWideAt = kStages * kStage, kCodeAt = kWideAt + kWides * kWide, kRings = kCodeAt + kCodes * kCode;
   static constexpr int kThreads = MODE == kForward ? 256 : 512;
-  static constexpr int kStaging = 4 * 32 * 33 * 4;                     // a warp's 32 x 32 results on their way out
-  static constexpr int kRings = kStages * kStage + kWides * kWide;
-  static constexpr size_t kSmem = 1024 + kRings + kStaging;
+  // PAIR: staging of results on their way out.  Otherwise a block's part of the results takes the rings' place at the end,
+  // rows of kRow floats.
+  static constexpr int kOut = PAIR ? 4 * (32 * 128 + (MODE == kForward ? 256 * 4 : 0)) : 0;
+  static constexpr int kRow = 132;
+  static_assert(PAIR || 128 * kRow * 4 <= kRings, "");
+  // two accumulators, one is read while the other is filled; PAIR false: and the sum of the pieces so far
+  static constexpr int kTmem = 512, kSum = 2 * kTile;
+  static constexpr size_t kSmem = 1024 + kRings + kOut;
+  static_assert(kSmem + 512 <= 227 * 1024, "");
 };
 
-// The order of the tiles: columns of 16 tiles high, so that the tiles in flight share their operands in L2.
-__device__ __forceinline__ void tile_at(int64_t t, int64_t tiles_m, int64_t tiles_n, int64_t& m, int64_t& n) {
-  constexpr int64_t kGroup = 16;
-  const int64_t per = kGroup * tiles_n, g = t / per, first = g * kGroup, high = min(kGroup, tiles_m - first), in = t - g * per;
-  m = first + in % high;
-  n = in / high;
+// The order of the tiles: columns of some 4096 rows high, so that the tiles in flight share their operands in L2.
+__device__ __forceinline__ void tile_at(int64_t t, int64_t high, int64_t tiles_m, int64_t tiles_n, int64_t& m, int64_t& n) {
+  const int64_t per = high * tiles_n, g = t / per, first = g * high, rows = min(high, tiles_m - first), in = t - g * per;
+  m = first + in % rows;
+  n = in / rows;
 }
 
 // Codes to bfloat16, times a scale.  The low seven bits of a code go into 128.0 (whose unit is 1), the sign bit into a second
@@ -169,231 +255,356 @@ __device__ __forceinline__ uint32_t restore2(uint32_t pair, __nv_bfloat162 scale
   const __nv_bfloat162 d = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&y)), scale);
   return *reinterpret_cast<const uint32_t*>(&d);
 }
+template <bool IN_BF16>
 __device__ __forceinline__ uint4 restore8(uint32_t w0, uint32_t w1, float scale) {
-  const uint32_t b = __float_as_uint(scale);
-  if ((b & 0xFFFFu) == 0) {
-    const uint32_t twice = __byte_perm(b, 0, 0x3232);
+  if constexpr (IN_BF16) {
+    const uint32_t twice = __byte_perm(__float_as_uint(scale), 0, 0x3232);
     const __nv_bfloat162 s = *reinterpret_cast<const __nv_bfloat162*>(&twice);
     return make_uint4(restore2(__byte_perm(w0, 0, 0x4140), s), restore2(__byte_perm(w0, 0, 0x4342), s),
                       restore2(__byte_perm(w1, 0, 0x4140), s), restore2(__byte_perm(w1, 0, 0x4342), s));
+  } else {
+    auto two = [&](uint32_t w) { return pack2(restore((int8_t)w, scale), restore((int8_t)(w >> 8), scale)); };
+    return make_uint4(two(w0), two(w0 >> 16), two(w1), two(w1 >> 16));
   }
-  auto two = [&](uint32_t w) { return pack2(restore((int8_t)w, scale), restore((int8_t)(w >> 8), scale)); };
-  return make_uint4(two(w0), two(w0 >> 16), two(w1), two(w1 >> 16));
 }
 
-template <int MODE, int BN, bool SPLIT>
-__global__ void __launch_bounds__(Shape<MODE, BN>::kThreads, 1)
-k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const GemmArgs g) {
-  using S = Shape<MODE, BN>;
-  constexpr int kTmem = SPLIT ? BN : 2 * BN;
+// ---- results out ---------------------------------------------------------------------------------------------------------
+// COUNT consecutive results of a row, in float32, to their place: `add`: on top of what is there, with one addition.
+template <int COUNT>
+__device__ __forceinline__ void put(const GemmArgs& g, int64_t row, int64_t col, bool add, const float (&v)[COUNT]) {
+  if (row >= g.rows || col >= g.cols) return;
+  const bool whole = g.vec && col + COUNT <= g.cols;
+  if (g.bf16) {
+    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(g.out) + row * g.ldo + col;
+    if (whole) {
+      uint32_t w[COUNT / 2];
+#pragma unroll
+      for (int i = 0; i < COUNT / 2; ++i) {
+        float a = v[2 * i], b = v[2 * i + 1];
+        if (add) {
+          float p, q;
+          unpack2(reinterpret_cast<const uint32_t*>(to)[i], p, q);
+          a = __fadd_rn(a, p);
+          b = __fadd_rn(b, q);
+        }
+        w[i] = pack2(a, b);
+      }
+      if constexpr (COUNT == 4) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+      else *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i)
+      if (col + i < g.cols) to[i] = __float2bfloat16_rn(add ? __fadd_rn(v[i], (float)to[i]) : v[i]);
+    return;
+  }
+  float* to = static_cast<float*>(g.out) + row * g.ldo + col;
+  if (whole) {
+#pragma unroll
+    for (int i = 0; i < COUNT; i += 4) {
+      float4 w = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+      if (add) {
+        const float4 o = *reinterpret_cast<const float4*>(to + i);
+        w = make_float4(__fadd_rn(w.x, o.x), __fadd_rn(w.y, o.y), __fadd_rn(w.z, o.z), __fadd_rn(w.w, o.w));
+      }
+      *reinterpret_cast<float4*>(to + i) = w;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i)
+    if (col + i < g.cols) to[i] = add ? __fadd_rn(v[i], to[i]) : v[i];
+}
+
+// Eight results that are bfloat16 already (nothing is added to them).
+__device__ __forceinline__ void put_bf16(const GemmArgs& g, int64_t row, int64_t col, uint4 w) {
+  if (row >= g.rows || col >= g.cols) return;
+  __nv_bfloat16* to = static_cast<__nv_bfloat16*>(g.out) + row * g.ldo + col;
+  if (g.vec && col + 8 <= g.cols) {
+    *reinterpret_cast<uint4*>(to) = w;
+    return;
+  }
+  const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (col + i < g.cols) reinterpret_cast<uint16_t*>(to)[i] = (uint16_t)(words[i / 2] >> (16 * (i & 1)));
+}
+
+template <int MODE, bool PAIR>
+__global__ void __launch_bounds__(Shape<MODE, PAIR>::kThreads, 1)
+k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_scales,
+          const GemmArgs g) {
+  using S = Shape<MODE, PAIR>;
   extern __shared__ unsigned char raw[];
-  __shared__ alignas(8) uint64_t bars[2 * S::kStages + 2 * S::kWides + 4];
+  __shared__ alignas(8) uint64_t bars[2 * (S::kStages + S::kCodes + S::kWides) + 4];
   __shared__ uint32_t tmem_slot;
   __shared__ int failed;
   const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
-  const uint32_t wide = ring + S::kStages * S::kStage;
   unsigned char* const ring_ptr = raw + (ring - smem_addr(raw));
-  const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, wide_full = empty + 8 * S::kStages,
-                 wide_empty = wide_full + 8 * S::kWides, acc_full = wide_empty + 8 * S::kWides, acc_empty = acc_full + 16;
+  // full: the operands that the tensor cores read from the stages have landed (PAIR: in both blocks; the first block's barrier
+  // counts).  codes_full, codes_empty: this block's codes.  wide_full, acc_empty: arrivals of both blocks, at the first one's.
+  const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, codes_full = empty + 8 * S::kStages, codes_empty = codes_full + 8 * S::kCodes,
+                 wide_full = codes_empty + 8 * S::kCodes, wide_empty = wide_full + 8 * S::kWides, acc_full = wide_empty + 8 * S::kWides,
+                 acc_empty = acc_full + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint32_t splits = 1, part = 0;
-  if constexpr (SPLIT) {
-    asm("mov.u32 %0, %cluster_nctarank;" : "=r"(splits));
-    asm("mov.u32 %0, %cluster_ctarank;" : "=r"(part));
-  }
+  uint32_t blocks, rank;
+  asm("mov.u32 %0, %cluster_nctarank;" : "=r"(blocks));
+  asm("mov.u32 %0, %cluster_ctarank;" : "=r"(rank));
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) {
       bar_init(full + 8 * i, 1);
       bar_init(empty + 8 * i, 1);
     }
+    for (int i = 0; i < S::kCodes; ++i) {
+      bar_init(codes_full + 8 * i, 1);
+      bar_init(codes_empty + 8 * i, S::kTurn);  // a warp each
+    }
     for (int i = 0; i < S::kWides; ++i) {
-      bar_init(wide_full + 8 * i, 256);
+      bar_init(wide_full + 8 * i, PAIR ? 2 * S::kTurn : S::kTurn);  // a warp each
       bar_init(wide_empty + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(acc_full + 8 * i, 1);
-      bar_init(acc_empty + 8 * i, 128);
+      bar_init(acc_empty + 8 * i, PAIR ? 8 : 4);
     }
     failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 2) tmem_alloc<kTmem>(smem_addr(&tmem_slot));
+  if (warp == 2) tmem_alloc<PAIR, S::kTmem>(smem_addr(&tmem_slot));
   tc_fence_before();
   __syncthreads();
+  if constexpr (PAIR) cluster_sync();  // the other block's barriers are there
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
+  if (threadIdx.x == 0) {
+    prefetch_map(&map_a);
+    prefetch_map(&map_b);
+    if constexpr (MODE != kForward) prefetch_map(&map_scales);
+  }
   pdl_wait();
   pdl_launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x == 0) *g.status = NSML_OK;
 
-  const int64_t tiles = g.tiles_m * g.tiles_n, first = blockIdx.x / splits, stride = gridDim.x / splits;
-  const int from = (int)((int64_t)g.steps * part / splits), to = (int)((int64_t)g.steps * (part + 1) / splits);
+  // PAIR: a cluster takes every so many-th tile.  Otherwise one tile, and this block a part of its sum.
+  const int64_t tiles = g.tiles_m * g.tiles_n, clusters = gridDim.x / blocks, first = blockIdx.x / blocks;
+  const int64_t high = PAIR ? 16 : 32, stride = PAIR ? clusters : tiles;
+  const int from = PAIR ? 0 : (int)((int64_t)g.steps * rank / blocks), to = PAIR ? g.steps : (int)((int64_t)g.steps * (rank + 1) / blocks);
 
-  if (warp == 0) {
-    if (elect_one()) {  // ---- loads
+  if (warp == 0 || (MODE != kForward && warp == 3)) {
+    if (elect_one()) {  // ---- loads: warp 0 what the tensor cores read, warp 3 codes
       uint32_t it = 0;
       bool ok = true;
       for (int64_t t = first; ok && t < tiles; t += stride) {
         int64_t m, n;
-        tile_at(t, g.tiles_m, g.tiles_n, m, n);
+        tile_at(t, high, g.tiles_m, g.tiles_n, m, n);
+        const int row = (int)(m * S::kTile + (PAIR ? rank * 128 : 0)), col = (int)(n * S::kTile + (PAIR ? rank * 128 : 0));
+        if (MODE != kForward && warp == 3) {
+          for (int k = from; k < to; ++k, ++it) {
+            const uint32_t s = it % S::kCodes, at = ring + S::kCodeAt + s * S::kCode, bar = codes_full + 8 * s;
+            if (!(ok = bar_wait(codes_empty + 8 * s, (it / S::kCodes + 1) & 1, &failed))) break;
+            bar_expect(bar, 128 * 64 + 68 * 4);
+            tma_load<false>(at, &map_b, col, k * 64, bar);
+            tma_load_1d(at + 128 * 64, &map_scales, k * 64, bar);
+          }
+          continue;
+        }
         for (int k = from; k < to; ++k, ++it) {
-          const uint32_t s = it % S::kStages, bar = full + 8 * s, at = ring + s * S::kStage;
+          const uint32_t s = it % S::kStages, at = ring + s * S::kStage;
           if (!(ok = bar_wait(empty + 8 * s, (it / S::kStages + 1) & 1, &failed))) break;
-          bar_expect(bar, S::kStage);
+          const uint32_t bar = PAIR ? in_block(full + 8 * s, 0) : full + 8 * s;
+          if (!PAIR || rank == 0) bar_expect(full + 8 * s, PAIR ? 2 * S::kStage : S::kStage);
           if constexpr (MODE == kForward) {
-            tma_load(at, &map_a, k * 128, (int)(m * kTileM), bar);
-            tma_load(at + S::kA, &map_b, k * 128, (int)(n * BN), bar);
+            tma_load<PAIR>(at, &map_a, k * 128, row, bar);
+            tma_load<PAIR>(at + 128 * 128, &map_b, k * 128, col, bar);
+          } else if constexpr (MODE == kGradInput) {
+            tma_load<PAIR>(at, &map_a, k * 64, row, bar);
           } else {
-            if constexpr (MODE == kGradInput) {
-              tma_load(at, &map_a, k * 64, (int)(m * kTileM), bar);
-            } else {
-              tma_load(at, &map_a, (int)(m * kTileM), k * 64, bar);
-              tma_load(at + S::kA / 2, &map_a, (int)(m * kTileM) + 64, k * 64, bar);
-            }
-            tma_load(at + S::kA, &map_b, (int)(n * BN), k * 64, bar);
+            tma_load<PAIR>(at, &map_a, row, k * 64, bar);
+            tma_load<PAIR>(at + 64 * 128, &map_a, row + 64, k * 64, bar);
           }
         }
       }
-      // copies in flight land before the block's shared memory goes (after a failure too: each wait is bounded)
-      if (!ok) {
-        for (uint32_t back = 0; back < S::kStages && back < it; ++back) {
-          const uint32_t i = it - 1 - back;
-          const unsigned long long began = now_ns();
-          while (!bar_try(full + 8 * (i % S::kStages), (i / S::kStages) & 1) && now_ns() - began < kWaitNs) {}
-        }
+      if (!ok) {  // copies in flight land before the block's shared memory goes; this wait is bounded too
+        const unsigned long long began = now_ns();
+        while (now_ns() - began < kWaitNs / 100) {}
       }
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (elect_one()) {  // ---- products
-      uint32_t it = 0, count = 0;
+    if ((!PAIR || rank == 0) && elect_one()) {  // ---- products
+      uint32_t it = 0, unit = 0;
       bool ok = true;
-      for (int64_t t = first; ok && t < tiles; t += stride, ++count) {
-        const uint32_t buffer = SPLIT ? 0 : count & 1, acc = tmem + buffer * BN;
-        if (!(ok = bar_wait(acc_empty + 8 * buffer, ((count >> 1) + 1) & 1, &failed))) break;
-        tc_fence_after();
-        for (int k = from; k < to; ++k, ++it) {
-          const uint32_t s = it % S::kStages, at = ring + s * S::kStage, w = it % S::kWides;
-          if (!(ok = bar_wait(full + 8 * s, (it / S::kStages) & 1, &failed))) break;
-          if constexpr (MODE != kForward)
-            if (!(ok = bar_wait(wide_full + 8 * w, (it / S::kWides) & 1, &failed))) break;
+      for (int64_t t = first; ok && t < tiles; t += stride) {
+        for (int piece = from; ok && piece < to; piece += g.piece, ++unit) {
+          const uint32_t buffer = unit & 1, acc = tmem + buffer * S::kTile;
+          if (!(ok = bar_wait_cluster(acc_empty + 8 * buffer, ((unit >> 1) + 1) & 1, &failed))) break;
           tc_fence_after();
+          const int end = min(to, piece + g.piece);
+          for (int k = piece; k < end; ++k, ++it) {
+            const uint32_t s = it % S::kStages, at = ring + s * S::kStage, w = it % S::kWides, wide = ring + S::kWideAt + w * S::kWide;
+            if (!(ok = bar_wait(full + 8 * s, (it / S::kStages) & 1, &failed))) break;
+            if constexpr (MODE != kForward)
+              if (!(ok = bar_wait_cluster(wide_full + 8 * w, (it / S::kWides) & 1, &failed))) break;
+            tc_fence_after();
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint64_t a = MODE == kGradWeight ? tile_desc(at + j * 2048, 8192, 1024) : tile_desc(at + j * 32, 16, 1024);
-            const uint64_t b = MODE == kForward ? tile_desc(at + S::kA + j * 32, 16, 1024) : tile_desc(wide + w * S::kWide + j * 2048, 8192, 1024);
-            tc_mma<MODE>(acc, a, b, mma_desc<MODE, BN>(), k > from || j > 0);
+            for (int j = 0; j < 4; ++j) {
+              const uint64_t a = MODE == kGradWeight ? tile_desc(at + j * 2048, 8192, 1024) : tile_desc(at + j * 32, 16, 1024);
+              const uint64_t b = MODE == kForward ? tile_desc(at + 128 * 128 + j * 32, 16, 1024) : tile_desc(wide + j * 2048, 8192, 1024);
+              tc_mma<MODE, PAIR>(acc, a, b, mma_desc<MODE, PAIR>(), k > piece || j > 0);
+            }
+            tc_commit<PAIR>(empty + 8 * s);
+            if constexpr (MODE != kForward) tc_commit<PAIR>(wide_empty + 8 * w);
           }
-          tc_commit(empty + 8 * s);
-          if constexpr (MODE != kForward) tc_commit(wide_empty + 8 * w);
+          if (ok) tc_commit<PAIR>(acc_full + 8 * buffer);
         }
-        if (ok) tc_commit(acc_full + 8 * buffer);
       }
     }
     __syncwarp();
   } else if (warp >= 4 && warp < 8) {  // ---- results
     const int quarter = warp - 4;
-    uint32_t* const stage = reinterpret_cast<uint32_t*>(ring_ptr + S::kRings) + quarter * 32 * 33;
-    uint32_t count = 0;
-    for (int64_t t = first; t < tiles; t += stride, ++count) {
-      const uint32_t buffer = SPLIT ? 0 : count & 1;
-      if (!bar_wait(acc_full + 8 * buffer, (count >> 1) & 1, &failed)) break;
-      tc_fence_after();
+    unsigned char* const out = ring_ptr + S::kRings;
+    uint32_t unit = 0;
+    bool ok = true;
+    for (int64_t t = first; ok && t < tiles; t += stride) {
       int64_t m, n;
-      tile_at(t, g.tiles_m, g.tiles_n, m, n);
-      const int64_t row0 = m * kTileM + quarter * 32;
-      const float my_scale = MODE == kForward && row0 + lane < g.rows ? g.row_scale[row0 + lane] : 0.0f;
-#pragma unroll 1
-      for (int c = 0; c < BN / 32; ++c) {
-        uint32_t r[32];
-        tmem_load32(tmem + buffer * BN + c * 32 + ((uint32_t)quarter << 21), r);
-        if (c == BN / 32 - 1) {
+      tile_at(t, high, g.tiles_m, g.tiles_n, m, n);
+      for (int piece = from; piece < to; piece += g.piece, ++unit) {
+        const uint32_t buffer = unit & 1, acc = tmem + buffer * S::kTile + ((uint32_t)quarter << 21);
+        if (!(ok = bar_wait(acc_full + 8 * buffer, (unit >> 1) & 1, &failed))) break;
+        tc_fence_after();
+        auto release = [&] {  // the accumulator has been read
           tc_fence_before();
-          bar_arrive(acc_empty + 8 * buffer);
-        }
-#pragma unroll
-        for (int j = 0; j < 32; ++j) stage[lane * 33 + j] = r[j];
-        __syncwarp();
-        // half a warp per row, two columns per lane
-        const int64_t col = n * BN + c * 32 + 2 * (lane & 15);
-        float cs[2] = {0.0f, 0.0f};
-        if constexpr (MODE == kForward) {
-          if (col < g.cols) cs[0] = g.col_scale[col];
-          if (col + 1 < g.cols) cs[1] = g.col_scale[col + 1];
-        }
-#pragma unroll 4
-        for (int i = 0; i < 16; ++i) {
-          const int rr = 2 * i + (lane >> 4);
-          const int64_t row = row0 + rr;
-          const uint32_t* from_stage = stage + rr * 33 + 2 * (lane & 15);
-          float v[2];
-          if constexpr (MODE == kForward) {
-            const float rs = __shfl_sync(0xFFFFFFFFu, my_scale, rr);
-            v[0] = __fmul_rn(__fmul_rn((float)(int)from_stage[0], rs), cs[0]);
-            v[1] = __fmul_rn(__fmul_rn((float)(int)from_stage[1], rs), cs[1]);
-          } else {
-            v[0] = __uint_as_float(from_stage[0]);
-            v[1] = __uint_as_float(from_stage[1]);
-          }
-          if (row >= g.rows || col >= g.cols) continue;
-          if (g.bf16) {
-            __nv_bfloat16* to_row = static_cast<__nv_bfloat16*>(g.out) + row * g.ldo + col;
-            if (g.pair && col + 1 < g.cols) {
-              if (g.add) {
-                float a, b;
-                unpack2(*reinterpret_cast<const uint32_t*>(to_row), a, b);
-                v[0] = __fadd_rn(v[0], a);
-                v[1] = __fadd_rn(v[1], b);
-              }
-              *reinterpret_cast<uint32_t*>(to_row) = pack2(v[0], v[1]);
-            } else {
-              for (int e = 0; e < 2 && col + e < g.cols; ++e)
-                to_row[e] = __float2bfloat16_rn(g.add ? __fadd_rn(v[e], (float)to_row[e]) : v[e]);
-            }
-          } else {
-            float* to_row = static_cast<float*>(g.out) + row * g.ldo + col;
-            for (int e = 0; e < 2 && col + e < g.cols; ++e) to_row[e] = g.add ? __fadd_rn(v[e], to_row[e]) : v[e];
-          }
-        }
-        __syncwarp();
-      }
-    }
-  } else if (MODE != kForward && warp >= 8) {  // ---- codes to bfloat16
-    if constexpr (MODE != kForward) {
-      constexpr int kLanes = BN / 16, kRowsAtOnce = 32 / kLanes, kRounds = 8 / kRowsAtOnce;  // a warp: 8 rows of a tile
-      const int sub = lane % kLanes, row = (warp - 8) * 8 + lane / kLanes;
-      const int flip = (sub >> 2) & 1;  // lanes whose blocks of columns share banks write their halves in opposite order
-      uint32_t it = 0;
-      bool ok = true;
-      for (int64_t t = first; ok && t < tiles; t += stride) {
-        float scale[kRounds];
-        auto fetch = [&](int k) {
-#pragma unroll
-          for (int i = 0; i < kRounds; ++i) {
-            const int64_t at = (int64_t)k * 64 + row + i * kRowsAtOnce;
-            scale[i] = k < to && at < g.depth ? g.depth_scale[at] : 0.0f;
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (PAIR) bar_arrive_cluster(in_block(acc_empty + 8 * buffer, 0));
+            else bar_arrive(acc_empty + 8 * buffer);
           }
         };
-        fetch(from);
-        for (int k = from; k < to; ++k, ++it) {
-          const uint32_t s = it % S::kStages, w = it % S::kWides;
-          if (!(ok = bar_wait(wide_empty + 8 * w, (it / S::kWides + 1) & 1, &failed))) break;
-          if (!(ok = bar_wait(full + 8 * s, (it / S::kStages) & 1, &failed))) break;
-          const unsigned char* codes = ring_ptr + s * S::kStage + S::kA;
-          unsigned char* dst = ring_ptr + S::kStages * S::kStage + w * S::kWide + (sub >> 2) * 8192;
-#pragma unroll
-          for (int i = 0; i < kRounds; ++i) {
-            const int rr = row + i * kRowsAtOnce;
-            const uint4 q = *reinterpret_cast<const uint4*>(codes + rr * BN + sub * 16);
-            const uint4 o[2] = {restore8(q.x, q.y, scale[i]), restore8(q.z, q.w, scale[i])};
-            unsigned char* line = dst + rr * 128;
-            const int c0 = (sub & 3) * 2;
-            *reinterpret_cast<uint4*>(line + (((c0 + flip) ^ (rr & 7)) << 4)) = flip ? o[1] : o[0];
-            *reinterpret_cast<uint4*>(line + (((c0 + 1 - flip) ^ (rr & 7)) << 4)) = flip ? o[0] : o[1];
+        if constexpr (PAIR) {
+          unsigned char* const stage = out + quarter * 4096;  // 32 rows of 128 bytes, pieces of 16 swizzled
+          float* const scales = reinterpret_cast<float*>(out + 4 * 4096) + quarter * 256;
+          const int64_t row0 = m * 256 + rank * 128 + quarter * 32, col0 = n * 256;
+          const bool add = g.add || piece > from, packed = g.bf16 && !add;
+          float rs = 0.0f;
+          if constexpr (MODE == kForward) {
+            rs = row0 + lane < g.rows ? g.row_scale[row0 + lane] : 0.0f;
+            for (int i = lane; i < 256; i += 32) scales[i] = col0 + i < g.cols ? g.col_scale[col0 + i] : 0.0f;
+            __syncwarp();
           }
-          fence_async_shared();
-          bar_arrive(wide_full + 8 * w);
-          fetch(k + 1);
+#pragma unroll 1
+          for (int c = 0; c < 8; ++c) {
+            uint32_t r[32];
+            tmem_load32(acc + c * 32, r);
+            if (c == 7) release();
+            if constexpr (MODE == kForward) {
+#pragma unroll
+              for (int j = 0; j < 32; j += 4) {
+                const float4 cs = *reinterpret_cast<const float4*>(scales + c * 32 + j);
+                r[j] = __float_as_uint(__fmul_rn(__fmul_rn((float)(int)r[j], rs), cs.x));
+                r[j + 1] = __float_as_uint(__fmul_rn(__fmul_rn((float)(int)r[j + 1], rs), cs.y));
+                r[j + 2] = __float_as_uint(__fmul_rn(__fmul_rn((float)(int)r[j + 2], rs), cs.z));
+                r[j + 3] = __float_as_uint(__fmul_rn(__fmul_rn((float)(int)r[j + 3], rs), cs.w));
+              }
+            }
+            unsigned char* const line = stage + lane * 128;
+            if (packed) {  // 64 columns of bfloat16 at a time
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                uint4 w;
+                w.x = pack2(__uint_as_float(r[8 * j]), __uint_as_float(r[8 * j + 1]));
+                w.y = pack2(__uint_as_float(r[8 * j + 2]), __uint_as_float(r[8 * j + 3]));
+                w.z = pack2(__uint_as_float(r[8 * j + 4]), __uint_as_float(r[8 * j + 5]));
+                w.w = pack2(__uint_as_float(r[8 * j + 6]), __uint_as_float(r[8 * j + 7]));
+                *reinterpret_cast<uint4*>(line + (((j + 4 * (c & 1)) ^ (lane & 7)) << 4)) = w;
+              }
+              if ((c & 1) == 0) continue;
+            } else {  // 32 columns of float32
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                *reinterpret_cast<uint4*>(line + ((j ^ (lane & 7)) << 4)) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int rr = 4 * i + (lane >> 3), j = lane & 7;
+              const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
+              if (packed) {
+                put_bf16(g, row0 + rr, col0 + (c >> 1) * 64 + 8 * j, w);
+              } else {
+                const float v[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
+                put<4>(g, row0 + rr, col0 + c * 32 + 4 * j, add, v);
+              }
+            }
+            __syncwarp();
+          }
+        } else {  // the sum of the pieces stays in TMEM; in the end it is this block's part (integers, or float32)
+          const bool last = piece + g.piece >= to;
+          float* const line = reinterpret_cast<float*>(ring_ptr) + (quarter * 32 + lane) * S::kRow;
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            uint32_t r[32];
+            tmem_load32(acc + c * 32, r);
+            if (c == 3) release();
+            const uint32_t sum = tmem + S::kSum + ((uint32_t)quarter << 21) + c * 32;
+            if (piece > from) {  // (never integers)
+              uint32_t o[32];
+              tmem_load32(sum, o);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__fadd_rn(__uint_as_float(o[j]), __uint_as_float(r[j])));
+            }
+            if (!last) {
+              tmem_store32(sum, r);
+              continue;
+            }
+            // (all of the block's products are done, so nothing reads or fills the rings any more)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(line + c * 32 + 4 * j) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+          }
+        }
+      }
+    }
+  } else if (MODE != kForward && warp >= 8) {  // ---- codes to bfloat16: the warps take turns at the steps, kTurn of them at one
+    if constexpr (MODE != kForward) {
+      constexpr int kTurn = S::kTurn, kTurns = S::kTurns, kRows = 64 / kTurn;
+      const int sub = lane & 7, row = (warp - 8) % kTurn * kRows + (lane >> 3);
+      const int flip = sub >> 2, c0 = (sub & 3) * 2;  // lanes whose blocks of columns share banks write their halves in opposite order
+      const int64_t mine = first < tiles ? (tiles - first + stride - 1) / stride : 0, total = mine * (to - from);
+      for (int64_t it = (warp - 8) / kTurn; it < total; it += kTurns) {
+        const uint32_t s = (uint32_t)(it % S::kCodes), w = (uint32_t)(it % S::kWides);
+        if (!bar_wait(codes_full + 8 * s, (uint32_t)(it / S::kCodes) & 1, &failed)) break;
+        const unsigned char* codes = ring_ptr + S::kCodeAt + s * S::kCode;
+        const float* scales = reinterpret_cast<const float*>(codes + 128 * 64) + g.scale_shift;
+        unsigned char* dst = ring_ptr + S::kWideAt + w * S::kWide + (sub >> 2) * 8192;
+        uint4 q[kRows / 4];
+        float scale[kRows / 4];
+        bool in_bf16 = true;
+#pragma unroll
+        for (int i = 0; i < kRows / 4; ++i) {
+          const int rr = row + 4 * i;
+          q[i] = *reinterpret_cast<const uint4*>(codes + rr * 128 + sub * 16);
+          scale[i] = scales[rr];
+          in_bf16 = in_bf16 && (__float_as_uint(scale[i]) & 0xFFFFu) == 0;
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(codes_empty + 8 * s);  // (they are in registers)
+        if (!bar_wait(wide_empty + 8 * w, ((uint32_t)(it / S::kWides) & 1) ^ 1, &failed)) break;
+        auto convert = [&](auto kind) {
+#pragma unroll
+          for (int i = 0; i < kRows / 4; ++i) {
+            const int rr = row + 4 * i;
+            const uint4 lo = restore8<kind>(q[i].x, q[i].y, scale[i]), hi = restore8<kind>(q[i].z, q[i].w, scale[i]);
+            unsigned char* line = dst + rr * 128;
+            *reinterpret_cast<uint4*>(line + (((c0 + flip) ^ (rr & 7)) << 4)) = flip ? hi : lo;
+            *reinterpret_cast<uint4*>(line + (((c0 + 1 - flip) ^ (rr & 7)) << 4)) = flip ? lo : hi;
+          }
+        };
+        if (__all_sync(0xFFFFFFFFu, in_bf16)) convert(std::true_type{});  // (one branch per step, so that its rows overlap)
+        else convert(std::false_type{});
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (PAIR) bar_arrive_cluster(in_block(wide_full + 8 * w, 0));
+          else bar_arrive(wide_full + 8 * w);
         }
       }
     }
@@ -401,9 +612,42 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
 
   tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  if (warp == 2) tmem_free<kTmem>(tmem);
   if (threadIdx.x == 0 && failed != 0) set_status(g.status, NSML_ERR_TIMEOUT);
+  cluster_sync();  // PAIR: neither block's memory is used by the other any more.  Otherwise: every block's part is complete
+  tc_fence_after();
+  if (warp == 2) tmem_free<PAIR, S::kTmem>(tmem);
+  if constexpr (!PAIR) {  // a warp per row of the tile, rows dealt out to the blocks
+    const uint32_t parts = ring;
+    int64_t m, n;
+    tile_at(first, high, g.tiles_m, g.tiles_n, m, n);
+    const int64_t col = n * 128 + 4 * lane;
+    float cs[4];
+    if constexpr (MODE == kForward) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) cs[i] = col + i < g.cols ? g.col_scale[col + i] : 0.0f;
+    }
+    for (int rr = rank + blocks * warp; rr < 128 && m * 128 + rr < g.rows; rr += blocks * (S::kThreads / 32)) {
+      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      int sum[4] = {0, 0, 0, 0};
+      for (uint32_t p = 0; p < blocks; ++p) {
+        uint32_t x[4];
+        asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                     : "r"(in_block(parts + (rr * S::kRow + 4 * lane) * 4, p)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (MODE == kForward) sum[i] += (int)x[i];
+          else v[i] = p == 0 ? __uint_as_float(x[i]) : __fadd_rn(v[i], __uint_as_float(x[i]));
+        }
+      }
+      if constexpr (MODE == kForward) {
+        const float rs = g.row_scale[m * 128 + rr];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __fmul_rn(__fmul_rn((float)sum[i], rs), cs[i]);
+      }
+      put<4>(g, m * 128 + rr, col, g.add, v);
+    }
+    cluster_sync();  // no block leaves while another reads its part
+  }
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
@@ -423,6 +667,15 @@ static EncodeTiled encoder() {  // found in the driver, so that the library need
   return f;
 }
 
+// `count` scales, from the 16-byte boundary at or before them; boxes of 68.
+static bool scales_map(CUtensorMap* map, const float* scales, int64_t count, int* shift) {
+  *shift = (int)(reinterpret_cast<uintptr_t>(scales) % 16 / 4);
+  const cuuint64_t dims[1] = {(cuuint64_t)(count + *shift)}, strides[1] = {0};
+  const cuuint32_t box[1] = {68}, step[1] = {1};
+  return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 1, const_cast<float*>(scales - *shift), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // rows x cols elements; boxes of box_cols x box_rows.  What lies outside reads as 0.
 static bool tensor_map(CUtensorMap* map, const void* p, bool codes, int64_t rows, int64_t cols, int64_t ld, int box_cols, int box_rows, bool swizzle) {
   const int size = codes ? 1 : 2;
@@ -436,42 +689,93 @@ static bool tensor_map(CUtensorMap* map, const void* p, bool codes, int64_t rows
 
 struct GemmDevice {
   bool ready = false;
-  int sms = 0;
+  int pairs[4] = {}, split[4] = {};  // resident clusters of 1, 2, 4, 8 blocks of the two forms (PAIR: of two)
 };
 static GemmDevice g_gemm_dev[64];
 static std::mutex g_gemm_mutex;
 
-template <int MODE, int BN, bool SPLIT>
-static cudaError_t prepare_kernel() {
-  return cudaFuncSetAttribute(k_q8_gemm<MODE, BN, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<MODE, BN>::kSmem);
+// clusters[s]: how many clusters of 2^s blocks are resident at once (at most what all three modes have)
+template <int MODE, bool PAIR>
+static cudaError_t prepare_kernel(int* clusters) {
+  cudaError_t e = cudaFuncSetAttribute(k_q8_gemm<MODE, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<MODE, PAIR>::kSmem);
+  for (int s = 0; s <= 3 && e == cudaSuccess; ++s) {
+    if (PAIR && s != 1) continue;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1 << s);
+    cfg.blockDim = dim3(Shape<MODE, PAIR>::kThreads);
+    cfg.dynamicSmemBytes = Shape<MODE, PAIR>::kSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1 << s;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int c = 0;
+    e = cudaOccupancyMaxActiveClusters(&c, k_q8_gemm<MODE, PAIR>, &cfg);
+    if (e == cudaSuccess && c < 1) e = cudaErrorUnknown;
+    if (clusters[s] == 0 || c < clusters[s]) clusters[s] = c;
+  }
+  return e;
 }
 
-static int gemm_device(int* sms) {
+static int gemm_device(const GemmDevice** out) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cuda_error();
   std::lock_guard<std::mutex> lock(g_gemm_mutex);
   GemmDevice& d = g_gemm_dev[dev];
   if (!d.ready) {
-    cudaError_t e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess) e = prepare_kernel<kForward, 256, false>();
-    if (e == cudaSuccess) e = prepare_kernel<kGradInput, 256, false>();
-    if (e == cudaSuccess) e = prepare_kernel<kGradWeight, 256, false>();
+    cudaError_t e = prepare_kernel<kForward, true>(d.pairs);
+    if (e == cudaSuccess) e = prepare_kernel<kGradInput, true>(d.pairs);
+    if (e == cudaSuccess) e = prepare_kernel<kGradWeight, true>(d.pairs);
+    if (e == cudaSuccess) e = prepare_kernel<kForward, false>(d.split);
+    if (e == cudaSuccess) e = prepare_kernel<kGradInput, false>(d.split);
+    if (e == cudaSuccess) e = prepare_kernel<kGradWeight, false>(d.split);
     if (e != cudaSuccess || encoder() == nullptr) return cuda_error();
     d.ready = true;
   }
-  *sms = d.sms;
+  *out = &d;
   return NSML_OK;
 }
 
-template <int MODE, int BN, bool SPLIT>
-static int launch_gemm(const CUtensorMap& map_a, const CUtensorMap& map_b, GemmArgs g, int sms, cudaStream_t st) {
-  using S = Shape<MODE, BN>;
-  g.tiles_m = (g.rows + kTileM - 1) / kTileM;
-  g.tiles_n = (g.cols + BN - 1) / BN;
+static int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Which form: the one that is done first by a count of microseconds.  Measured on one B200, per call: a step of the sum takes
+// about a third of a microsecond in both forms while it waits for loads (a step of a 256 x 256 tile on two SMs takes as long
+// as one of a 128 x 128 tile on one), a wave of blocks six to seven besides its steps, the exchange of the parts one.
+// Returns the blocks per tile that share the sum, or 0: PAIR.
+static int choose_form(const GemmArgs& g, const GemmDevice& dev, double step_us) {
+  double best = 7.0 + (double)up(up(g.rows, 256) * up(g.cols, 256), dev.pairs[1]) * (g.steps * step_us * 1.2 + 0.3);
+  const int64_t tiles = up(g.rows, 128) * up(g.cols, 128);
+  int form = 0;
+  if (tiles > 4096) return form;
+  for (int s = 0; s <= 3 && (1 << s) <= g.steps; ++s) {
+    const double t = (double)up(tiles, dev.split[s]) * (6.0 + (s > 0 ? 1.0 : 0.0) + (double)up(g.steps, 1 << s) * step_us);
+    if (t < best) {
+      best = t;
+      form = 1 << s;
+    }
+  }
+  return form;
+}
+
+template <int MODE>
+static int launch_gemm(const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_scales, GemmArgs g, const GemmDevice& dev, cudaStream_t st) {
+  const int form = choose_form(g, dev, MODE == kForward ? 0.30 : 0.36);
+  const int tile = form == 0 ? 256 : 128;
+  g.tiles_m = up(g.rows, tile);
+  g.tiles_n = up(g.cols, tile);
   const int64_t tiles = g.tiles_m * g.tiles_n;
   LaunchScope scope(K_Q8_GEMM, st);
-  const cudaError_t e = launch_prio(k_q8_gemm<MODE, BN, SPLIT>, dim3((unsigned int)(tiles < sms ? tiles : sms)), dim3(S::kThreads), S::kSmem, st, false, 0,
-                                    false, true, map_a, map_b, g);
+  cudaError_t e;
+  if (form == 0) {
+    using S = Shape<MODE, true>;
+    e = launch_prio(k_q8_gemm<MODE, true>, dim3((unsigned int)(2 * (tiles < dev.pairs[1] ? tiles : dev.pairs[1]))), dim3(S::kThreads), S::kSmem, st, false, 2,
+                    false, true, map_a, map_b, map_scales, g);
+  } else {
+    using S = Shape<MODE, false>;
+    e = launch_prio(k_q8_gemm<MODE, false>, dim3((unsigned int)(tiles * form)), dim3(S::kThreads), S::kSmem, st, false, (unsigned int)form, false, true,
+                    map_a, map_b, map_scales, g);
+  }
   return e == cudaSuccess ? NSML_OK : cuda_error();
 }
 
@@ -496,7 +800,7 @@ static GemmArgs result(void* out, int64_t rows, int64_t cols, int64_t ldo, int d
   g.ldo = ldo;
   g.bf16 = dtype == NSML_BF16;
   g.add = add;
-  g.pair = g.bf16 && aligned(out, 4) && (rows <= 1 || ldo % 2 == 0);
+  g.vec = aligned(out, 16) && (rows <= 1 || ldo % (g.bf16 ? 8 : 4) == 0);
   g.status = static_cast<int*>(workspace);
   return g;
 }
@@ -517,16 +821,17 @@ int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const in
     return NSML_ERR_ARG;
   int rc = check_out(out, m, n, ldo, dtype, workspace, workspace_bytes);
   if (rc != NSML_OK) return rc;
-  int sms = 0;
-  if ((rc = gemm_device(&sms)) != NSML_OK) return rc;
+  const GemmDevice* dev = nullptr;
+  if ((rc = gemm_device(&dev)) != NSML_OK) return rc;
   GemmArgs g = result(out, m, n, ldo, dtype, false, workspace);
   g.row_scale = a_scales;
   g.col_scale = b_scales;
   g.depth = k;
   g.steps = (int)((k + 127) / 128);
+  g.piece = g.steps;
   CUtensorMap map_a, map_b;
-  if (!tensor_map(&map_a, a, true, m, k, lda, 128, kTileM, true) || !tensor_map(&map_b, b, true, n, k, ldb, 128, 256, true)) return NSML_ERR_CUDA;
-  return launch_gemm<kForward, 256, false>(map_a, map_b, g, sms, static_cast<cudaStream_t>(stream));
+  if (!tensor_map(&map_a, a, true, m, k, lda, 128, 128, true) || !tensor_map(&map_b, b, true, n, k, ldb, 128, 128, true)) return NSML_ERR_CUDA;
+  return launch_gemm<kForward>(map_a, map_b, map_b, g, *dev, static_cast<cudaStream_t>(stream));
 }
 
 int nsml_q8_matmul_grad_input(const void* dy, int64_t ldy, const int8_t* b, int64_t ldb, const float* b_scales, int64_t m, int64_t n, int64_t k,
@@ -536,15 +841,15 @@ int nsml_q8_matmul_grad_input(const void* dy, int64_t ldy, const int8_t* b, int6
   if (!valid_gradient(dy, m, n, ldy) || !valid_codes(b, n, k, ldb) || b_scales == nullptr || !aligned(b_scales, 4)) return NSML_ERR_ARG;
   int rc = check_out(dx, m, k, lddx, dtype, workspace, workspace_bytes);
   if (rc != NSML_OK) return rc;
-  int sms = 0;
-  if ((rc = gemm_device(&sms)) != NSML_OK) return rc;
+  const GemmDevice* dev = nullptr;
+  if ((rc = gemm_device(&dev)) != NSML_OK) return rc;
   GemmArgs g = result(dx, m, k, lddx, dtype, false, workspace);
-  g.depth_scale = b_scales;
   g.depth = n;
   g.steps = (int)((n + 63) / 64);
-  CUtensorMap map_a, map_b;
-  if (!tensor_map(&map_a, dy, false, m, n, ldy, 64, kTileM, true) || !tensor_map(&map_b, b, true, n, k, ldb, 256, 64, false)) return NSML_ERR_CUDA;
-  return launch_gemm<kGradInput, 256, false>(map_a, map_b, g, sms, static_cast<cudaStream_t>(stream));
+  g.piece = g.bf16 ? g.steps : kStepsPerPiece;
+  CUtensorMap map_a, map_b, map_scales;
+  if (!scales_map(&map_scales, b_scales, n, &g.scale_shift) || !tensor_map(&map_a, dy, false, m, n, ldy, 64, 128, true) || !tensor_map(&map_b, b, true, n, k, ldb, 128, 64, false)) return NSML_ERR_CUDA;
+  return launch_gemm<kGradInput>(map_a, map_b, map_scales, g, *dev, static_cast<cudaStream_t>(stream));
 }
 
 int nsml_q8_matmul_grad_weight(const void* dy, int64_t ldy, const int8_t* a, int64_t lda, const float* a_scales, int64_t m, int64_t n, int64_t k,
@@ -560,15 +865,15 @@ int nsml_q8_matmul_grad_weight(const void* dy, int64_t ldy, const int8_t* a, int
     if (zero_first && cudaMemset2DAsync(dw, (size_t)(n > 1 ? lddw : k) * size, 0, (size_t)k * size, (size_t)n, st) != cudaSuccess) return cuda_error();
     return NSML_OK;
   }
-  int sms = 0;
-  if ((rc = gemm_device(&sms)) != NSML_OK) return rc;
+  const GemmDevice* dev = nullptr;
+  if ((rc = gemm_device(&dev)) != NSML_OK) return rc;
   GemmArgs g = result(dw, n, k, lddw, dtype, zero_first == 0, workspace);
-  g.depth_scale = a_scales;
   g.depth = m;
   g.steps = (int)((m + 63) / 64);
-  CUtensorMap map_a, map_b;
-  if (!tensor_map(&map_a, dy, false, m, n, ldy, 64, 64, true) || !tensor_map(&map_b, a, true, m, k, lda, 256, 64, false)) return NSML_ERR_CUDA;
-  return launch_gemm<kGradWeight, 256, false>(map_a, map_b, g, sms, st);
+  g.piece = g.bf16 ? g.steps : kStepsPerPiece;
+  CUtensorMap map_a, map_b, map_scales;
+  if (!scales_map(&map_scales, a_scales, m, &g.scale_shift) || !tensor_map(&map_a, dy, false, m, n, ldy, 64, 64, true) || !tensor_map(&map_b, a, true, m, k, lda, 128, 64, false)) return NSML_ERR_CUDA;
+  return launch_gemm<kGradWeight>(map_a, map_b, map_scales, g, *dev, st);
 }
 
 }  // extern "C"
