@@ -9,6 +9,7 @@
 #include <cuda_bf16.h>
 
 #include "nsml_common.cuh"
+#include "nsml_launch.h"
 
 namespace nsml {
 namespace q8 {
@@ -29,19 +30,45 @@ __device__ __forceinline__ float scale_of(uint32_t amax_bits, float* inv) {
   return __uint_as_float((uint32_t)(127 + e) << 23);
 }
 
-// v is finite, or inv is 0 (codes of a row with NaN or infinity are 0)
-__device__ __forceinline__ int code_of(float v, float inv) {
-  const int c = inv == 0.0f ? 0 : __float2int_rn(__fmul_rn(v, inv));
-  return max(-127, min(127, c));
+// Four codes of values times inv (exact: a power of two).  Adding 1.5 * 2^23 rounds to an integer, half to even, whose low
+// byte is the code.  clamp: products may round to 128 (a scale held at 2^121), or the row is not finite (inv is 0: codes 0).
+__device__ __forceinline__ bool needs_clamp(uint32_t amax_bits) { return amax_bits >= 0x7EFF0000u; }  // 127.5 * 2^121
+template <bool CLAMP>
+__device__ __forceinline__ uint32_t code_bits(float v, float inv) {
+  if constexpr (CLAMP) {
+    const int c = inv == 0.0f ? 0 : __float2int_rn(__fmul_rn(v, inv));
+    return (uint32_t)max(-127, min(127, c));
+  }
+  return __float_as_uint(__fmaf_rn(v, inv, 12582912.0f));
+}
+template <bool CLAMP>
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+  return __byte_perm(__byte_perm(code_bits<CLAMP>(a, inv), code_bits<CLAMP>(b, inv), 0x0040),
+                     __byte_perm(code_bits<CLAMP>(c, inv), code_bits<CLAMP>(d, inv), 0x0040), 0x5410);
+}
+template <bool CLAMP>
+__device__ __forceinline__ uint2 codes8(const float (&v)[8], float inv) {
+  return make_uint2(codes4<CLAMP>(v[0], v[1], v[2], v[3], inv), codes4<CLAMP>(v[4], v[5], v[6], v[7], inv));
+}
+// largest magnitude so far; a NaN stays
+__device__ __forceinline__ float top3(float top, float a, float b) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(top), "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float top8(float top, const float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) top = top3(top, v[j], v[j + 1]);
+  return top;
 }
 
 __device__ __forceinline__ float restore(int code, float scale) { return __fmul_rn((float)code, scale); }
 
 // ---- eight consecutive elements ---------------------------------------------------------------------------------------
 template <int DTYPE>
-struct Elem { using type = float; };
+struct Elem { using type = float; using bits = uint32_t; };
 template <>
-struct Elem<NSML_BF16> { using type = __nv_bfloat16; };
+struct Elem<NSML_BF16> { using type = __nv_bfloat16; using bits = uint16_t; };
 
 __device__ __forceinline__ void unpack2(uint32_t w, float& a, float& b) {
   a = __uint_as_float(w << 16);
@@ -52,78 +79,175 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// Elements c .. c+7 of a row of `cols`; those past the end are 0.  vec: the row starts on a 16-byte boundary.
-template <int DTYPE>
-__device__ __forceinline__ void load8(const typename Elem<DTYPE>::type* row, int64_t c, int64_t cols, bool vec, float (&v)[8]) {
-  if (vec && c + 8 <= cols) {
-    if constexpr (DTYPE == NSML_F32) {
-      const float4 a = *reinterpret_cast<const float4*>(row + c), b = *reinterpret_cast<const float4*>(row + c + 4);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-      const uint4 a = *reinterpret_cast<const uint4*>(row + c);
-      unpack2(a.x, v[0], v[1]); unpack2(a.y, v[2], v[3]);
-      unpack2(a.z, v[4], v[5]); unpack2(a.w, v[6], v[7]);
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? (float)row[c + i] : 0.0f;
+// Eight elements of a row as they are in memory (four registers of bfloat16, eight of float32): chunk `i` of the thread that
+// is number `lane` of a row's THREADS.
+//   VEC      rows (and the width: a multiple of eight) are on 16-byte boundaries: eight consecutive elements
+//   else     every THREADS-th element, so that a warp's loads of one element each are next to each other
+// Elements past the end are 0, and are not written.
+template <bool VEC, int THREADS>
+__device__ __forceinline__ unsigned int column(int lane, int i, int j) {  // (past the end of the widest row it passes 2^31)
+  return VEC ? 8u * (lane + i * THREADS) + j : (8u * i + j) * THREADS + lane;
 }
+// whether chunk i of every thread lies past the end, or inside
+template <int THREADS>
+__device__ __forceinline__ bool outside(int i, int cols) { return 8u * i * THREADS >= (unsigned int)cols; }
+template <int THREADS>
+__device__ __forceinline__ bool inside(int i, int cols) { return 8u * i * THREADS + 8 * THREADS <= (unsigned int)cols; }
 
 template <int DTYPE>
-__device__ __forceinline__ void store8(typename Elem<DTYPE>::type* row, int64_t c, int64_t cols, bool vec, const float (&v)[8]) {
-  if (vec && c + 8 <= cols) {
+struct Raw8 {
+  uint4 w[DTYPE == NSML_F32 ? 2 : 1];
+  __device__ __forceinline__ void widen(float (&v)[8]) const {
     if constexpr (DTYPE == NSML_F32) {
-      *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      v[0] = __uint_as_float(w[0].x); v[1] = __uint_as_float(w[0].y); v[2] = __uint_as_float(w[0].z); v[3] = __uint_as_float(w[0].w);
+      v[4] = __uint_as_float(w[1].x); v[5] = __uint_as_float(w[1].y); v[6] = __uint_as_float(w[1].z); v[7] = __uint_as_float(w[1].w);
     } else {
-      *reinterpret_cast<uint4*>(row + c) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+      unpack2(w[0].x, v[0], v[1]); unpack2(w[0].y, v[2], v[3]);
+      unpack2(w[0].z, v[4], v[5]); unpack2(w[0].w, v[6], v[7]);
     }
-    return;
   }
+  __device__ __forceinline__ void round(const float (&v)[8]) {
+    if constexpr (DTYPE == NSML_F32) {
+      w[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+      w[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    } else {
+      w[0] = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+    }
+  }
+  // bits of element j
+  __device__ __forceinline__ void put(int j, uint32_t bits) {
+    if constexpr (DTYPE == NSML_F32) (&w[j / 4].x)[j % 4] = bits;
+    else (&w[0].x)[j / 2] = (j & 1) ? __byte_perm((&w[0].x)[j / 2], bits, 0x5410) : bits;
+  }
+  __device__ __forceinline__ uint32_t bits(int j) const {
+    if constexpr (DTYPE == NSML_F32) return (&w[j / 4].x)[j % 4];
+    return (j & 1) ? (&w[0].x)[j / 2] >> 16 : (&w[0].x)[j / 2];
+  }
+  using Bits = typename Elem<DTYPE>::bits;
+  template <bool VEC, int THREADS>
+  __device__ __forceinline__ void load(const typename Elem<DTYPE>::type* row, int lane, int i, int cols) {
+    w[0] = make_uint4(0, 0, 0, 0);
+    if constexpr (DTYPE == NSML_F32) w[1] = w[0];
+    if constexpr (VEC) {
+      if (column<VEC, THREADS>(lane, i, 0) >= (unsigned int)cols) return;
+      const uint4* from = reinterpret_cast<const uint4*>(row + column<VEC, THREADS>(lane, i, 0));
+      w[0] = from[0];
+      if constexpr (DTYPE == NSML_F32) w[1] = from[1];
+    } else {
+      const Bits* from = reinterpret_cast<const Bits*>(row) + lane;
+      if (inside<THREADS>(i, cols)) {  // (the offsets are the instructions' own)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) put(j, from[(8u * i + j) * THREADS]);
+      } else if (!outside<THREADS>(i, cols)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) put(j, column<VEC, THREADS>(lane, i, j) < (unsigned int)cols ? (uint32_t)from[(8u * i + j) * THREADS] : 0u);
+      }
+    }
+  }
+  template <bool VEC, int THREADS>
+  __device__ __forceinline__ void store(typename Elem<DTYPE>::type* row, int lane, int i, int cols) const {
+    if constexpr (VEC) {
+      if (column<VEC, THREADS>(lane, i, 0) >= (unsigned int)cols) return;
+      uint4* to = reinterpret_cast<uint4*>(row + column<VEC, THREADS>(lane, i, 0));
+      to[0] = w[0];
+      if constexpr (DTYPE == NSML_F32) to[1] = w[1];
+    } else {
+      Bits* to = reinterpret_cast<Bits*>(row) + lane;
+      if (inside<THREADS>(i, cols)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) to[(8u * i + j) * THREADS] = (Bits)bits(j);
+      } else if (!outside<THREADS>(i, cols)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (column<VEC, THREADS>(lane, i, j) < (unsigned int)cols) to[(8u * i + j) * THREADS] = (Bits)bits(j);
+      }
+    }
+  }
+};
+
+template <int DTYPE, bool VEC, int THREADS>
+__device__ __forceinline__ void load8(const typename Elem<DTYPE>::type* row, int lane, int i, int cols, float (&v)[8]) {
+  Raw8<DTYPE> r;
+  r.template load<VEC, THREADS>(row, lane, i, cols);
+  r.widen(v);
+}
+template <int DTYPE, bool VEC, int THREADS>
+__device__ __forceinline__ void store8(typename Elem<DTYPE>::type* row, int lane, int i, int cols, const float (&v)[8]) {
+  Raw8<DTYPE> r;
+  r.round(v);
+  r.template store<VEC, THREADS>(row, lane, i, cols);
+}
+
+// The same for codes, whose rows are always on 16-byte boundaries.
+template <bool VEC, int THREADS>
+__device__ __forceinline__ void store8_codes(int8_t* row, int lane, int i, int cols, uint2 w) {
+  if constexpr (VEC) {
+    if (column<VEC, THREADS>(lane, i, 0) < (unsigned int)cols) *reinterpret_cast<uint2*>(row + column<VEC, THREADS>(lane, i, 0)) = w;
+  } else {
+    int8_t* to = row + lane;
+    if (inside<THREADS>(i, cols)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) to[(8u * i + j) * THREADS] = (int8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+    } else if (!outside<THREADS>(i, cols)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (column<VEC, THREADS>(lane, i, j) < (unsigned int)cols) to[(8u * i + j) * THREADS] = (int8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+    }
+  }
+}
+template <bool VEC, int THREADS>
+__device__ __forceinline__ uint2 load8_codes(const int8_t* row, int lane, int i, int cols) {
+  uint2 w = make_uint2(0, 0);
+  if constexpr (VEC) {
+    if (column<VEC, THREADS>(lane, i, 0) < (unsigned int)cols) w = *reinterpret_cast<const uint2*>(row + column<VEC, THREADS>(lane, i, 0));
+  } else {
+    const uint8_t* from = reinterpret_cast<const uint8_t*>(row) + lane;
+    uint32_t b[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (inside<THREADS>(i, cols)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) b[j] = from[(8u * i + j) * THREADS];
+    } else if (!outside<THREADS>(i, cols)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) b[j] = column<VEC, THREADS>(lane, i, j) < (unsigned int)cols ? from[(8u * i + j) * THREADS] : 0;
+    }
+    w.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+    w.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+  }
+  return w;
+}
+
+// whether a row's threads skip chunk i (VEC: empty ones are only skipped where they are loaded and stored)
+template <bool VEC, int THREADS>
+__device__ __forceinline__ bool empty(int i, int cols) { return !VEC && outside<THREADS>(i, cols); }
+
+template <bool VEC, int THREADS>
+__device__ __forceinline__ void load8_weight(const void* weight, bool bf16, int lane, int i, int cols, float (&w)[8]) {
+  if (bf16) load8<NSML_BF16, VEC, THREADS>(static_cast<const __nv_bfloat16*>(weight), lane, i, cols, w);
+  else load8<NSML_F32, VEC, THREADS>(static_cast<const float*>(weight), lane, i, cols, w);
+}
+
+template <int THREADS>
+__device__ __forceinline__ int my_lane() { return threadIdx.x % THREADS; }
+
+// Codes as numbers: the byte, moved up by 128, becomes the last one of 2^23 (whose unit is 1).
+__device__ __forceinline__ void numbers8(uint2 w, float (&v)[8]) {
+  const uint32_t x = w.x ^ 0x80808080u, y = w.y ^ 0x80808080u;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (c + i < cols) row[c + i] = (typename Elem<DTYPE>::type)v[i];
+    v[i] = __fadd_rn(__uint_as_float(__byte_perm(i < 4 ? x : y, 0x4B000000u, 0x7540 | (i & 3))), -8388736.0f);
+}
+__device__ __forceinline__ void restore8_codes(uint2 w, float scale, float (&v)[8]) {
+  numbers8(w, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], scale);
 }
 
-// Eight codes; rows of codes start on 16-byte boundaries.  Nothing past `cols` is written.
-__device__ __forceinline__ void store8_codes(int8_t* row, int64_t c, int64_t cols, const int (&q)[8]) {
-  if (c + 8 <= cols) {
-    uint2 w;
-    w.x = (q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | q[3] << 24;
-    w.y = (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | q[7] << 24;
-    *reinterpret_cast<uint2*>(row + c) = w;
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (c + i < cols) row[c + i] = (int8_t)q[i];
-}
-
-// Restored values of eight codes; those past the end are 0 (whatever the bytes behind the row hold).
-__device__ __forceinline__ void load8_codes(const int8_t* row, int64_t c, int64_t cols, float scale, float (&v)[8]) {
-  if (c >= cols) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-    return;
-  }
-  // (c is a multiple of 8 and rows are a multiple of 16 bytes apart: the eight bytes are inside the row's own)
-  const uint2 w = *reinterpret_cast<const uint2*>(row + c);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int code = (int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
-    v[i] = c + i < cols ? restore(code, scale) : 0.0f;
-  }
-}
-
-// ---- sums over the THREADS threads that share a row (a warp, or the whole block) -----------------------------------------
+// ---- over the THREADS threads that share a row (part of a warp, a warp, or the whole block; then once per `shared`) --------
 template <int THREADS>
 __device__ __forceinline__ double row_sum(double v, double* shared) {
 #pragma unroll
-  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  for (int d = (THREADS < 32 ? THREADS : 32) / 2; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
   if constexpr (THREADS > 32) {
-    __syncthreads();
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
     __syncthreads();
     v = shared[0];
@@ -133,11 +257,17 @@ __device__ __forceinline__ double row_sum(double v, double* shared) {
   return v;
 }
 
+// bits of the largest magnitude (NaN's are above infinity's)
 template <int THREADS>
-__device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* shared) {
-  v = __reduce_max_sync(0xFFFFFFFFu, v);
+__device__ __forceinline__ uint32_t row_top(float top, uint32_t* shared) {
+  uint32_t v = __float_as_uint(top) & 0x7FFFFFFFu;
+  if constexpr (THREADS < 32) {
+#pragma unroll
+    for (int d = THREADS / 2; d; d >>= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+  } else {
+    v = __reduce_max_sync(0xFFFFFFFFu, v);
+  }
   if constexpr (THREADS > 32) {
-    __syncthreads();
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
     __syncthreads();
     v = shared[0];
@@ -145,6 +275,21 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* shared) {
     for (int w = 1; w < THREADS / 32; ++w) v = max(v, shared[w]);
   }
   return v;
+}
+
+// ---- arguments -----------------------------------------------------------------------------------------------------
+inline bool rows16(const void* p, int64_t ld, int dtype) {
+  return aligned(p, 16) && (ld * (dtype == NSML_F32 ? 4 : 2)) % 16 == 0;
+}
+inline bool valid_type(int dtype) { return dtype == NSML_F32 || dtype == NSML_BF16; }
+inline bool valid_matrix(const void* p, int64_t rows, int64_t cols, int64_t ld, int dtype) {
+  return p != nullptr && aligned(p, dtype == NSML_F32 ? 4 : 2) && (rows <= 1 || ld >= cols);
+}
+inline bool valid_codes(const void* p, int64_t rows, int64_t cols, int64_t ldq) {
+  return p != nullptr && aligned(p, 16) && (rows <= 1 || (ldq >= cols && ldq % 16 == 0));
+}
+inline bool valid_sizes(int64_t rows, int64_t cols, int64_t max_cols) {
+  return rows >= 0 && rows <= NSML_Q8_MAX_ROWS && cols >= 1 && cols <= max_cols;
 }
 
 }  // namespace q8

@@ -780,8 +780,8 @@ static int launch_gemm(const CUtensorMap& map_a, const CUtensorMap& map_b, const
 }
 
 static bool valid_size(int64_t v) { return v >= 0 && v <= NSML_Q8_MAX_ROWS; }
-static bool valid_codes(const void* p, int64_t rows, int64_t cols, int64_t ld) {
-  return p != nullptr && aligned(p, 16) && (rows <= 1 || (ld >= cols && ld % 16 == 0 && ld < ((int64_t)1 << 40)));
+static bool valid_operand(const void* p, int64_t rows, int64_t cols, int64_t ld) {
+  return valid_codes(p, rows, cols, ld) && (rows <= 1 || ld < ((int64_t)1 << 40));  // (the longest stride of a tensor map)
 }
 static bool valid_gradient(const void* p, int64_t rows, int64_t cols, int64_t ld) {
   return p != nullptr && aligned(p, 16) && (rows <= 1 || (ld >= cols && ld % 8 == 0 && ld < ((int64_t)1 << 39)));
@@ -817,7 +817,7 @@ int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const in
                    int64_t n, int64_t k, void* out, int64_t ldo, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (!valid_size(m) || !valid_size(n) || n < 1 || k < 1 || k > NSML_Q8_MAX_DEPTH) return NSML_ERR_ARG;
   if (m == 0) return NSML_OK;
-  if (!valid_codes(a, m, k, lda) || !valid_codes(b, n, k, ldb) || a_scales == nullptr || !aligned(a_scales, 4) || b_scales == nullptr || !aligned(b_scales, 4))
+  if (!valid_operand(a, m, k, lda) || !valid_operand(b, n, k, ldb) || a_scales == nullptr || !aligned(a_scales, 4) || b_scales == nullptr || !aligned(b_scales, 4))
     return NSML_ERR_ARG;
   int rc = check_out(out, m, n, ldo, dtype, workspace, workspace_bytes);
   if (rc != NSML_OK) return rc;
@@ -838,7 +838,7 @@ int nsml_q8_matmul_grad_input(const void* dy, int64_t ldy, const int8_t* b, int6
                               void* dx, int64_t lddx, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (!valid_size(m) || !valid_size(n) || !valid_size(k) || n < 1 || k < 1) return NSML_ERR_ARG;
   if (m == 0) return NSML_OK;
-  if (!valid_gradient(dy, m, n, ldy) || !valid_codes(b, n, k, ldb) || b_scales == nullptr || !aligned(b_scales, 4)) return NSML_ERR_ARG;
+  if (!valid_gradient(dy, m, n, ldy) || !valid_operand(b, n, k, ldb) || b_scales == nullptr || !aligned(b_scales, 4)) return NSML_ERR_ARG;
   int rc = check_out(dx, m, k, lddx, dtype, workspace, workspace_bytes);
   if (rc != NSML_OK) return rc;
   const GemmDevice* dev = nullptr;
@@ -855,7 +855,7 @@ int nsml_q8_matmul_grad_input(const void* dy, int64_t ldy, const int8_t* b, int6
 int nsml_q8_matmul_grad_weight(const void* dy, int64_t ldy, const int8_t* a, int64_t lda, const float* a_scales, int64_t m, int64_t n, int64_t k,
                                void* dw, int64_t lddw, int dtype, int zero_first, void* workspace, size_t workspace_bytes, void* stream) {
   if (!valid_size(m) || !valid_size(n) || !valid_size(k) || n < 1 || k < 1) return NSML_ERR_ARG;
-  if (m > 0 && (!valid_gradient(dy, m, n, ldy) || !valid_codes(a, m, k, lda) || a_scales == nullptr || !aligned(a_scales, 4))) return NSML_ERR_ARG;
+  if (m > 0 && (!valid_gradient(dy, m, n, ldy) || !valid_operand(a, m, k, lda) || a_scales == nullptr || !aligned(a_scales, 4))) return NSML_ERR_ARG;
   int rc = check_out(dw, n, k, lddw, dtype, workspace, workspace_bytes);
   if (rc != NSML_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
