@@ -247,10 +247,11 @@ def nsml_accumulate_workspace_bytes(n: int, W: int) -> int:
 # --------------------------------------------------------------------------
 _torch_module = None
 _raw_stream = None  # () -> the current stream as an integer
+_device_index = None  # () -> the current device's index (0 where there is no device)
 
 
 def _torch():
-    global _torch_module, _raw_stream
+    global _torch_module, _raw_stream, _device_index
     if _torch_module is None:
         import torch
 
@@ -260,6 +261,8 @@ def _torch():
             _raw_stream = lambda: get(device())  # noqa: E731
         else:
             _raw_stream = lambda: int(torch.cuda.current_stream().cuda_stream)  # noqa: E731
+        # (without a device every tensor is refused by its own index, -1)
+        _device_index = (device or torch.cuda.current_device) if torch.cuda.is_available() else lambda: 0
         _torch_module = torch
     return _torch_module
 
@@ -521,28 +524,31 @@ NSML_Q8_MATMUL_WORKSPACE_BYTES = 256
 
 def _matrix(t, what: str, rows: Optional[int] = None, cols: Optional[int] = None, dtype=None):
     """Checks a 2-D CUDA tensor of the current device with contiguous rows; returns (pointer, row stride)."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise ValueError(f"{what} must have shape ({rows}, {cols}), not {tuple(t.shape)}")
+    if (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+        raise ValueError(f"{what} must have shape ({rows}, {cols}), not {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
-    _on_current_device(t, what)
-    return t.data_ptr(), t.stride(0)
+    if t.get_device() != _current_device():
+        raise ValueError(f"{what} must be a tensor of the current CUDA device")
+    return t.data_ptr(), stride[0]
 
 
 def _vector(t, what: str, n: int, dtype=None):
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.shape != (n,) or (n > 1 and t.stride()[0] != 1):
         raise ValueError(f"{what} must be a contiguous 1-D tensor of {n} elements")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
-    _on_current_device(t, what)
+    if t.get_device() != _current_device():
+        raise ValueError(f"{what} must be a tensor of the current CUDA device")
     return t.data_ptr()
 
 
-def _on_current_device(t, what: str) -> None:
-    if not t.is_cuda or t.device.index != _torch().cuda.current_device():
-        raise ValueError(f"{what} must be a tensor of the current CUDA device")
+def _current_device() -> int:
+    _torch()
+    return _device_index()
 
 
 def _q8_dtype(dtype) -> int:
@@ -557,7 +563,8 @@ def _q8_dtype(dtype) -> int:
 def _workspace(workspace, nbytes: int, device):
     if workspace is None:
         return alloc_bytes(nbytes, device)
-    _on_current_device(workspace, "workspace")
+    if workspace.get_device() != _current_device():
+        raise ValueError("workspace must be a tensor of the current CUDA device")
     return workspace
 
 

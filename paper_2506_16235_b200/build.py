@@ -17,13 +17,13 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG_DIR, "libnsml.so")
 STAMP_PATH = LIB_PATH + ".stamp"
 
-SOURCES = ["nsml_api.cu", "nsml_grid_large.cu", "nsml_q8_rows.cu", "nsml_q8_norm_grad.cu", "nsml_q8_gemm.cu", "nsml_controller.cpp"]
+SOURCES = ["nsml_api.cu", "nsml_grid_large.cu", "nsml_q8_rows.cu", "nsml_q8_norm_grad.cu", "nsml_q8_gemm.cu", "nsml_q8_tokens.cu", "nsml_controller.cpp"]
 FLAGS = [
     "-O3", "-std=c++17", "-lineinfo",
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-ftz=false", "-prec-div=true", "-prec-sqrt=true", "-fmad=false",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-ffp-contract=off",
-    "-shared", "-cudart", "static", "--threads", "6",
+    "-shared", "-cudart", "static", "--threads", "7",
 ]
 
 

@@ -23,6 +23,7 @@
 
 #include "nsml_launch.h"
 #include "nsml_q8.cuh"
+#include "nsml_q8_products.h"
 
 namespace nsml {
 namespace q8 {
@@ -821,6 +822,9 @@ int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const in
     return NSML_ERR_ARG;
   int rc = check_out(out, m, n, ldo, dtype, workspace, workspace_bytes);
   if (rc != NSML_OK) return rc;
+  if (m <= kMaxTokens)
+    return launch_tokens(a, lda, a_scales, b, ldb, b_scales, (int)m, n, (int)k, out, ldo, dtype == NSML_BF16, static_cast<int*>(workspace),
+                         static_cast<cudaStream_t>(stream));
   const GemmDevice* dev = nullptr;
   if ((rc = gemm_device(&dev)) != NSML_OK) return rc;
   GemmArgs g = result(out, m, n, ldo, dtype, false, workspace);
