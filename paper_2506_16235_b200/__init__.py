@@ -524,46 +524,48 @@ NSML_Q8_MATMUL_WORKSPACE_BYTES = 256
 
 def _matrix(t, what: str, rows: Optional[int] = None, cols: Optional[int] = None, dtype=None):
     """Checks a 2-D CUDA tensor of the current device with contiguous rows; returns (pointer, row stride)."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+    if t.dim() != 2:
         raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
-    if (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
-        raise ValueError(f"{what} must have shape ({rows}, {cols}), not {tuple(shape)}")
-    if dtype is not None and t.dtype != dtype:
+    (r, c), (ld, inner) = t.shape, t.stride()
+    if inner != 1 and c > 1:
+        raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        raise ValueError(f"{what} must have shape ({rows}, {cols}), not ({r}, {c})")
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
-    if t.get_device() != _current_device():
+    if t.get_device() != (_device_index or _device_query())():
         raise ValueError(f"{what} must be a tensor of the current CUDA device")
-    return t.data_ptr(), stride[0]
+    return t.data_ptr(), ld
 
 
 def _vector(t, what: str, n: int, dtype=None):
-    if t.shape != (n,) or (n > 1 and t.stride()[0] != 1):
+    if t.dim() != 1 or t.numel() != n or (n > 1 and not t.is_contiguous()):
         raise ValueError(f"{what} must be a contiguous 1-D tensor of {n} elements")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
-    if t.get_device() != _current_device():
+    if t.get_device() != (_device_index or _device_query())():
         raise ValueError(f"{what} must be a tensor of the current CUDA device")
     return t.data_ptr()
 
 
-def _current_device() -> int:
+def _device_query():
     _torch()
-    return _device_index()
+    return _device_index
 
 
 def _q8_dtype(dtype) -> int:
-    torch = _torch()
-    if dtype == torch.float32:
-        return NSML_F32
-    if dtype == torch.bfloat16:
+    torch = _torch_module or _torch()
+    if dtype is torch.bfloat16:
         return NSML_BF16
+    if dtype is torch.float32:
+        return NSML_F32
     raise TypeError("matrices must be float32 or bfloat16")
 
 
 def _workspace(workspace, nbytes: int, device):
     if workspace is None:
         return alloc_bytes(nbytes, device)
-    if workspace.get_device() != _current_device():
+    if workspace.get_device() != _device_query()():
         raise ValueError("workspace must be a tensor of the current CUDA device")
     return workspace
 

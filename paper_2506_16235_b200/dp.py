@@ -146,3 +146,59 @@ class GradientExchange:
             lambda views: nsml.nsml_decompress_accumulate(views, dense, zero_first=True, workspace=self.aws, sized=True),
             on_cuda=True, group=self.group)
         return self.ratio
+
+
+class NormLinear:
+    """A linear layer behind an RMS norm, trained in 8 bits, whose gradients land where the exchange takes them from:
+
+        y = rms_norm(x + residual) @ weight.T
+
+    The forward pass normalises into 8-bit rows, multiplies them with the 8-bit weights and keeps, for the backward pass, those
+    rows, the reciprocal norms and the residual stream in 8 bits: two bytes per element.  The backward pass writes the gradients
+    of the norm's weight and of the weight into bucket[offset : offset + size], ready for GradientExchange.step.  CUDA only.
+
+    weight [n, k] and norm_weight [k]: float32 or bfloat16 tensors that the optimiser owns; call pack() after it has changed
+    them.  bucket: flat float32 or bfloat16 gradient bucket."""
+
+    @staticmethod
+    def size(n: int, k: int) -> int:
+        """Elements of the bucket that the layer's gradients take: the norm's weight, then the weight."""
+        return k + n * k
+
+    def __init__(self, weight: torch.Tensor, norm_weight: torch.Tensor, bucket: torch.Tensor, offset: int = 0, eps: float = 1e-5):
+        import paper_2506_16235_b200 as nsml
+
+        n, k = weight.shape
+        if offset < 0 or offset + self.size(n, k) > bucket.numel():
+            raise ValueError(f"the bucket has no room for {self.size(n, k)} gradients at {offset}")
+        self.nsml, self.weight, self.norm_weight, self.eps = nsml, weight, norm_weight, float(eps)
+        self.grad_norm_weight = bucket[offset:offset + k]
+        self.grad_weight = bucket[offset + k:offset + k + n * k].view(n, k)
+        self.codes, self.scales = nsml.nsml_q8_empty(n, k, weight.device)
+        self.workspace = nsml.alloc_bytes(max(nsml.NSML_Q8_MATMUL_WORKSPACE_BYTES, int(nsml.lib.nsml_q8_rms_norm_backward_workspace_bytes(k))),
+                                          weight.device)
+        self.kept = None
+        self.pack()
+
+    def pack(self) -> None:
+        """8-bit weights from the weights as they are now."""
+        self.nsml.nsml_q8_pack(self.weight, codes=self.codes, scales=self.scales)
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor = None):
+        """x, residual [m, k] -> y [m, n] of x's type and h = x + residual (x itself without a residual)."""
+        rows, scales, rstd, h = self.nsml.nsml_q8_rms_norm(x, self.norm_weight, self.eps, residual=residual)
+        self.kept = rows, scales, rstd, self.nsml.nsml_q8_pack(h)
+        return self.nsml.nsml_q8_matmul(rows, scales, self.codes, self.scales, dtype=x.dtype, workspace=self.workspace), h
+
+    def backward(self, dy: torch.Tensor, dh: torch.Tensor = None, zero_first: bool = True) -> torch.Tensor:
+        """dy [m, n] (bfloat16, n a multiple of 8): writes (zero_first=False: adds) the weights' gradients and returns the
+        gradient of x and residual (bfloat16), dh (a gradient that reaches h past the norm) included.  Frees what the forward
+        pass kept."""
+        if self.kept is None:
+            raise RuntimeError("backward() without a forward() before it")
+        (rows, scales, rstd, (h_codes, h_scales)), self.kept = self.kept, None
+        nsml = self.nsml
+        nsml.nsml_q8_matmul_grad_weight(dy, rows, scales, dw=self.grad_weight, zero_first=zero_first, workspace=self.workspace)
+        dnormed = nsml.nsml_q8_matmul_grad_input(dy, self.codes, self.scales, workspace=self.workspace)
+        return nsml.nsml_q8_rms_norm_backward(dnormed, self.norm_weight, rstd, codes=h_codes, scales=h_scales, dh=dh, dx=dnormed,
+                                              dweight=self.grad_norm_weight, zero_first=zero_first, workspace=self.workspace)[0]
