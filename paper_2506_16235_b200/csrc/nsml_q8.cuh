@@ -79,10 +79,12 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// Eight elements of a row as they are in memory (four registers of bfloat16, eight of float32): chunk `i` of the thread that
-// is number `lane` of a row's THREADS.
-//   VEC      rows (and the width: a multiple of eight) are on 16-byte boundaries: eight consecutive elements
+// Eight elements of a row as they are in memory: chunk `i` of the thread that is number `lane` of a row's THREADS.
+//   VEC      rows (and the width: a multiple of eight) are on 16-byte boundaries: eight consecutive elements, four registers
+//            of bfloat16 or eight of float32
 //   else     every THREADS-th element, so that a warp's loads of one element each are next to each other
+//   APART    of those: a register each, so that they are waited for where they are used (putting two together waits where they
+//            are loaded, but takes half the registers)
 // Elements past the end are 0, and are not written.
 template <bool VEC, int THREADS>
 __device__ __forceinline__ unsigned int column(int lane, int i, int j) {  // (past the end of the widest row it passes 2^31)
@@ -94,45 +96,38 @@ __device__ __forceinline__ bool outside(int i, int cols) { return 8u * i * THREA
 template <int THREADS>
 __device__ __forceinline__ bool inside(int i, int cols) { return 8u * i * THREADS + 8 * THREADS <= (unsigned int)cols; }
 
-template <int DTYPE>
+template <int DTYPE, bool VEC, bool APART = false>
 struct Raw8 {
-  uint4 w[DTYPE == NSML_F32 ? 2 : 1];
+  static constexpr bool kPairs = (VEC || !APART) && DTYPE == NSML_BF16;
+  uint32_t w[kPairs ? 4 : 8];
   __device__ __forceinline__ void widen(float (&v)[8]) const {
-    if constexpr (DTYPE == NSML_F32) {
-      v[0] = __uint_as_float(w[0].x); v[1] = __uint_as_float(w[0].y); v[2] = __uint_as_float(w[0].z); v[3] = __uint_as_float(w[0].w);
-      v[4] = __uint_as_float(w[1].x); v[5] = __uint_as_float(w[1].y); v[6] = __uint_as_float(w[1].z); v[7] = __uint_as_float(w[1].w);
+    if constexpr (kPairs) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) unpack2(w[j], v[2 * j], v[2 * j + 1]);
     } else {
-      unpack2(w[0].x, v[0], v[1]); unpack2(w[0].y, v[2], v[3]);
-      unpack2(w[0].z, v[4], v[5]); unpack2(w[0].w, v[6], v[7]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(DTYPE == NSML_F32 ? w[j] : w[j] << 16);
     }
   }
   __device__ __forceinline__ void round(const float (&v)[8]) {
-    if constexpr (DTYPE == NSML_F32) {
-      w[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-      w[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    if constexpr (kPairs) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = pack2(v[2 * j], v[2 * j + 1]);
     } else {
-      w[0] = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = DTYPE == NSML_F32 ? __float_as_uint(v[j]) : (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
     }
   }
-  // bits of element j
-  __device__ __forceinline__ void put(int j, uint32_t bits) {
-    if constexpr (DTYPE == NSML_F32) (&w[j / 4].x)[j % 4] = bits;
-    else (&w[0].x)[j / 2] = (j & 1) ? __byte_perm((&w[0].x)[j / 2], bits, 0x5410) : bits;
-  }
-  __device__ __forceinline__ uint32_t bits(int j) const {
-    if constexpr (DTYPE == NSML_F32) return (&w[j / 4].x)[j % 4];
-    return (j & 1) ? (&w[0].x)[j / 2] >> 16 : (&w[0].x)[j / 2];
-  }
   using Bits = typename Elem<DTYPE>::bits;
-  template <bool VEC, int THREADS>
+  template <int THREADS>
   __device__ __forceinline__ void load(const typename Elem<DTYPE>::type* row, int lane, int i, int cols) {
-    w[0] = make_uint4(0, 0, 0, 0);
-    if constexpr (DTYPE == NSML_F32) w[1] = w[0];
+#pragma unroll
+    for (uint32_t& x : w) x = 0;
     if constexpr (VEC) {
       if (column<VEC, THREADS>(lane, i, 0) >= (unsigned int)cols) return;
       const uint4* from = reinterpret_cast<const uint4*>(row + column<VEC, THREADS>(lane, i, 0));
-      w[0] = from[0];
-      if constexpr (DTYPE == NSML_F32) w[1] = from[1];
+      set(0, from[0]);
+      if constexpr (!kPairs) set(4, from[1]);
     } else {
       const Bits* from = reinterpret_cast<const Bits*>(row) + lane;
       if (inside<THREADS>(i, cols)) {  // (the offsets are the instructions' own)
@@ -144,13 +139,13 @@ struct Raw8 {
       }
     }
   }
-  template <bool VEC, int THREADS>
+  template <int THREADS>
   __device__ __forceinline__ void store(typename Elem<DTYPE>::type* row, int lane, int i, int cols) const {
     if constexpr (VEC) {
       if (column<VEC, THREADS>(lane, i, 0) >= (unsigned int)cols) return;
       uint4* to = reinterpret_cast<uint4*>(row + column<VEC, THREADS>(lane, i, 0));
-      to[0] = w[0];
-      if constexpr (DTYPE == NSML_F32) to[1] = w[1];
+      to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      if constexpr (!kPairs) to[1] = make_uint4(w[4], w[5], w[6], w[7]);
     } else {
       Bits* to = reinterpret_cast<Bits*>(row) + lane;
       if (inside<THREADS>(i, cols)) {
@@ -163,19 +158,33 @@ struct Raw8 {
       }
     }
   }
+  __device__ __forceinline__ void put(int j, uint32_t x) {
+    if constexpr (kPairs) w[j / 2] = (j & 1) ? __byte_perm(w[j / 2], x, 0x5410) : x;
+    else w[j] = x;
+  }
+  __device__ __forceinline__ uint32_t bits(int j) const {
+    if constexpr (kPairs) return (j & 1) ? w[j / 2] >> 16 : w[j / 2];
+    else return w[j];
+  }
+  __device__ __forceinline__ void set(int at, const uint4& x) {
+    w[at] = x.x;
+    w[at + 1] = x.y;
+    w[at + 2] = x.z;
+    w[at + 3] = x.w;
+  }
 };
 
 template <int DTYPE, bool VEC, int THREADS>
 __device__ __forceinline__ void load8(const typename Elem<DTYPE>::type* row, int lane, int i, int cols, float (&v)[8]) {
-  Raw8<DTYPE> r;
-  r.template load<VEC, THREADS>(row, lane, i, cols);
+  Raw8<DTYPE, VEC> r;
+  r.template load<THREADS>(row, lane, i, cols);
   r.widen(v);
 }
 template <int DTYPE, bool VEC, int THREADS>
 __device__ __forceinline__ void store8(typename Elem<DTYPE>::type* row, int lane, int i, int cols, const float (&v)[8]) {
-  Raw8<DTYPE> r;
+  Raw8<DTYPE, VEC> r;
   r.round(v);
-  r.template store<VEC, THREADS>(row, lane, i, cols);
+  r.template store<THREADS>(row, lane, i, cols);
 }
 
 // The same for codes, whose rows are always on 16-byte boundaries.
@@ -195,26 +204,48 @@ __device__ __forceinline__ void store8_codes(int8_t* row, int lane, int i, int c
     }
   }
 }
-template <bool VEC, int THREADS>
-__device__ __forceinline__ uint2 load8_codes(const int8_t* row, int lane, int i, int cols) {
-  uint2 w = make_uint2(0, 0);
-  if constexpr (VEC) {
-    if (column<VEC, THREADS>(lane, i, 0) < (unsigned int)cols) w = *reinterpret_cast<const uint2*>(row + column<VEC, THREADS>(lane, i, 0));
-  } else {
-    const uint8_t* from = reinterpret_cast<const uint8_t*>(row) + lane;
-    uint32_t b[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (inside<THREADS>(i, cols)) {
+template <bool VEC, bool APART = false>
+struct RawCodes8 {
+  static constexpr bool kFours = VEC || !APART;
+  uint32_t w[kFours ? 2 : 8];
+  template <int THREADS>
+  __device__ __forceinline__ void load(const int8_t* row, int lane, int i, int cols) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) b[j] = from[(8u * i + j) * THREADS];
-    } else if (!outside<THREADS>(i, cols)) {
+    for (uint32_t& x : w) x = 0;
+    if constexpr (VEC) {
+      if (column<VEC, THREADS>(lane, i, 0) >= (unsigned int)cols) return;
+      const uint2 x = *reinterpret_cast<const uint2*>(row + column<VEC, THREADS>(lane, i, 0));
+      w[0] = x.x;
+      w[1] = x.y;
+    } else {
+      const uint8_t* from = reinterpret_cast<const uint8_t*>(row) + lane;
+      uint32_t b[8] = {};
+      if (inside<THREADS>(i, cols)) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) b[j] = column<VEC, THREADS>(lane, i, j) < (unsigned int)cols ? from[(8u * i + j) * THREADS] : 0;
+        for (int j = 0; j < 8; ++j) b[j] = from[(8u * i + j) * THREADS];
+      } else if (!outside<THREADS>(i, cols)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b[j] = column<VEC, THREADS>(lane, i, j) < (unsigned int)cols ? (uint32_t)from[(8u * i + j) * THREADS] : 0u;
+      }
+      if constexpr (kFours) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          w[j] = __byte_perm(__byte_perm(b[4 * j], b[4 * j + 1], 0x0040), __byte_perm(b[4 * j + 2], b[4 * j + 3], 0x0040), 0x5410);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = b[j];
+      }
     }
-    w.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-    w.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
   }
-  return w;
-}
+  // As numbers: the byte, moved up by 128, becomes the last one of 2^23 (whose unit is 1).
+  __device__ __forceinline__ void numbers(float (&v)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t bits = kFours ? __byte_perm(w[kFours ? j / 4 : 0] ^ 0x80808080u, 0x4B000000u, 0x7540 | (j & 3)) : (w[kFours ? 0 : j] ^ 0x80u) | 0x4B000000u;
+      v[j] = __fadd_rn(__uint_as_float(bits), -8388736.0f);
+    }
+  }
+};
 
 // whether a row's threads skip chunk i (VEC: empty ones are only skipped where they are loaded and stored)
 template <bool VEC, int THREADS>
@@ -228,19 +259,6 @@ __device__ __forceinline__ void load8_weight(const void* weight, bool bf16, int 
 
 template <int THREADS>
 __device__ __forceinline__ int my_lane() { return threadIdx.x % THREADS; }
-
-// Codes as numbers: the byte, moved up by 128, becomes the last one of 2^23 (whose unit is 1).
-__device__ __forceinline__ void numbers8(uint2 w, float (&v)[8]) {
-  const uint32_t x = w.x ^ 0x80808080u, y = w.y ^ 0x80808080u;
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    v[i] = __fadd_rn(__uint_as_float(__byte_perm(i < 4 ? x : y, 0x4B000000u, 0x7540 | (i & 3))), -8388736.0f);
-}
-__device__ __forceinline__ void restore8_codes(uint2 w, float scale, float (&v)[8]) {
-  numbers8(w, v);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], scale);
-}
 
 // ---- over the THREADS threads that share a row (part of a warp, a warp, or the whole block; then once per `shared`) --------
 template <int THREADS>

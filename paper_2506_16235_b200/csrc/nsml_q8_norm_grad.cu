@@ -34,10 +34,10 @@ constexpr int kGradBlock = 256;
 template <int THREADS>
 __host__ __device__ constexpr int grad_block() { return THREADS < kGradBlock ? kGradBlock : THREADS; }
 
-template <int DTYPE>
-__device__ __forceinline__ void forget(Raw8<DTYPE>& r) {  // the compiler is not to keep what it has worked out from r
+template <class Raw>
+__device__ __forceinline__ void forget(Raw& r) {  // the compiler is not to keep what it has worked out from r
 #pragma unroll
-  for (uint4& w : r.w) asm volatile("" : "+r"(w.x), "+r"(w.y), "+r"(w.z), "+r"(w.w));
+  for (uint32_t& w : r.w) asm volatile("" : "+r"(w));
 }
 
 template <int BYTES>
@@ -49,7 +49,7 @@ __device__ __forceinline__ void copy_async(void* to, const void* from) {
 // Where a thread's chunks of the next row wait: two sets of dy, h (or codes) and dh.
 template <int DTYPE, bool VEC, int THREADS, int CHUNKS>
 struct GradStage {
-  static constexpr int kPiece = sizeof(Raw8<DTYPE>);
+  static constexpr int kPiece = sizeof(Raw8<DTYPE, true>);
   static constexpr size_t kSet = (size_t)3 * CHUNKS * kPiece * grad_block<THREADS>();
   static constexpr bool kAhead = VEC && 2 * kSet * (THREADS <= kGradBlock ? 2 : 1) <= 200 * 1024;  // (of two blocks, where an SM has two)
   static constexpr size_t kSum = THREADS < kGradBlock ? (size_t)kGradBlock * CHUNKS * 32 : 0;       // the rows' parts of dweight, in the end
@@ -77,10 +77,10 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
   for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
-  Raw8<DTYPE> weight[KEEP ? CHUNKS : 1];
+  Raw8<DTYPE, VEC> weight[KEEP ? CHUNKS : 1];
   if constexpr (KEEP)
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) weight[i].template load<VEC, THREADS>(static_cast<const T*>(a.weight), lane, i, a.cols);
+    for (int i = 0; i < CHUNKS; ++i) weight[i].template load<THREADS>(static_cast<const T*>(a.weight), lane, i, a.cols);
   auto weights = [&](int i, float (&w)[8]) {
     if constexpr (KEEP) weight[i].widen(w);
     else load8_weight<VEC, THREADS>(a.weight, a.weight_bf16, lane, i, a.cols, w);
@@ -122,35 +122,67 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
       if (column<VEC, THREADS>(lane, i, 0) >= (unsigned int)a.cols)
         for (int k = 0; k < 6 * G::kPiece; k += 16) *reinterpret_cast<uint4*>(place(k / (3 * G::kPiece), k / G::kPiece % 3, i) + k % G::kPiece) = make_uint4(0, 0, 0, 0);
   }
+  // rows that cannot be copied 16 bytes at a time: the next one is loaded into registers meanwhile, where they suffice
+  constexpr bool kNext = !G::kAhead && THREADS <= 512;
+  struct {
+    Raw8<DTYPE, VEC, true> dy[CHUNKS], dh[CHUNKS], h[PACKED ? 1 : CHUNKS];
+    RawCodes8<VEC, true> codes[PACKED ? CHUNKS : 1];
+  } next;
+  auto load = [&](int64_t at, auto& to) {
+    const int end = at < a.rows ? a.cols : 0;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      to.dy[i].template load<THREADS>(static_cast<const T*>(a.dy) + at * a.ldy, lane, i, end);
+      if constexpr (PACKED) to.codes[i].template load<THREADS>(a.codes + at * a.ldq, lane, i, end);
+      else to.h[i].template load<THREADS>(static_cast<const T*>(a.h) + at * a.ldh, lane, i, end);
+      if (a.dh != nullptr) to.dh[i].template load<THREADS>(static_cast<const T*>(a.dh) + at * a.lddh, lane, i, end);
+    }
+  };
   float rstd_next, factor_next;
   scalars(row, rstd_next, factor_next);
   ahead(0, row);
+  if constexpr (kNext) load(row, next);
   for (int64_t turn = 0; turn < turns; ++turn, row += step) {
     const int set = (int)(turn & 1), end = row < a.rows ? a.cols : 0;
     const float rstd = rstd_next, factor = __fmul_rn(factor_next, rstd);
-    Raw8<DTYPE> dy[CHUNKS], dh[CHUNKS], h[PACKED ? 1 : CHUNKS];
-    uint2 codes[PACKED ? CHUNKS : 1];
+    Raw8<DTYPE, VEC, true> dy[CHUNKS], dh[CHUNKS], h[PACKED ? 1 : CHUNKS];
+    RawCodes8<VEC, true> codes[PACKED ? CHUNKS : 1];
     ahead(set ^ 1, row + step);
     scalars(row + step, rstd_next, factor_next);
     if constexpr (G::kAhead) {
       asm volatile("cp.async.wait_group 1;" ::: "memory");
     } else {
+      if constexpr (!kNext) load(row, next);
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
-        dy[i].template load<VEC, THREADS>(static_cast<const T*>(a.dy) + row * a.ldy, lane, i, end);
-        if constexpr (PACKED) codes[i] = load8_codes<VEC, THREADS>(a.codes + row * a.ldq, lane, i, end);
-        else h[i].template load<VEC, THREADS>(static_cast<const T*>(a.h) + row * a.ldh, lane, i, end);
-        if (a.dh != nullptr) dh[i].template load<VEC, THREADS>(static_cast<const T*>(a.dh) + row * a.lddh, lane, i, end);
+        dy[i] = next.dy[i];
+        dh[i] = next.dh[i];
+        if constexpr (PACKED) codes[i] = next.codes[i];
+        else h[i] = next.h[i];
       }
+      if constexpr (kNext) load(row + step, next);
     }
-    auto fetched = [&](int o, int i, const Raw8<DTYPE>& direct, float (&v)[8]) {
-      if constexpr (G::kAhead) reinterpret_cast<const Raw8<DTYPE>*>(place(set, o, i))->widen(v);
+    auto fetched = [&](int o, int i, const Raw8<DTYPE, VEC, true>& direct, float (&v)[8]) {
+      if constexpr (G::kAhead) {
+        const uint4* p = reinterpret_cast<const uint4*>(place(set, o, i));
+        Raw8<DTYPE, VEC> x;
+        x.set(0, p[0]);
+        if constexpr (DTYPE == NSML_F32) x.set(4, p[1]);
+        x.widen(v);
+      }
       else direct.widen(v);
     };
     auto kept = [&](int i, float (&v)[8]) {
-      if constexpr (!PACKED) fetched(1, i, h[i], v);
-      else if constexpr (G::kAhead) numbers8(*reinterpret_cast<const uint2*>(place(set, 1, i)), v);
-      else numbers8(codes[i], v);
+      if constexpr (!PACKED) {
+        fetched(1, i, h[i], v);
+      } else {
+        if constexpr (G::kAhead) {
+          const uint2 x = *reinterpret_cast<const uint2*>(place(set, 1, i));
+          codes[i].w[0] = x.x;
+          codes[i].w[1] = x.y;
+        }
+        codes[i].numbers(v);
+      }
     };
     float dot = 0.0f;
     if (row < a.rows)
@@ -183,7 +215,7 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
         forget(dy[i]);
-        if constexpr (PACKED) asm volatile("" : "+r"(codes[i].x), "+r"(codes[i].y));
+        if constexpr (PACKED) forget(codes[i]);
         else forget(h[i]);
       }
     }
@@ -253,16 +285,17 @@ __global__ void __launch_bounds__(1024) k_q8_norm_weight(const float* __restrict
   }
 }
 
-// The gradient of the norm: threads per row (32 columns each, of float32 16), and blocks: what a B200's 148 SMs hold; also the
-// height of the workspace's table.
-static int grad_threads(int64_t cols, int dtype) {
-  const int64_t each = dtype == NSML_F32 ? 16 : 32;
-  int threads = dtype == NSML_F32 ? 8 : 4;
+// The gradient of the norm: chunks per thread, threads per row, and blocks: what a B200's 148 SMs hold; also the height of the
+// workspace's table.
+static constexpr int grad_chunks(int dtype, bool vec) { return vec ? (dtype == NSML_F32 ? 2 : 4) : 1; }
+static int grad_threads(int64_t cols, int dtype, bool vec) {
+  const int64_t each = 8 * grad_chunks(dtype, vec);
+  int threads = 128 / (int)each;  // narrowest: 128 columns
   while (threads < 1024 && cols > each * threads) threads *= (threads < 32 ? 4 : 2);
   return threads;
 }
-static int grad_blocks(int64_t rows, int64_t cols, int dtype) {
-  const int threads = grad_threads(cols, dtype), teams = threads < kGradBlock ? kGradBlock / threads : 1;
+static int grad_blocks(int64_t rows, int64_t cols, int dtype, bool vec) {
+  const int threads = grad_threads(cols, dtype, vec), teams = threads < kGradBlock ? kGradBlock / threads : 1;
   const int64_t most = threads <= kGradBlock ? 2 * 148 : 148, need = (rows + teams - 1) / teams;
   return (int)(need < most ? need : most);
 }
@@ -277,18 +310,17 @@ static int norm_grad_rows(const NormGradArgs& a, cudaStream_t st) {
                                      : cudaSuccess;
     if (e != cudaSuccess) return cuda_error();
     LaunchScope scope(K_Q8_NORM_GRAD, st);
-    e = launch_prio(k_q8_norm_grad<DTYPE, PACKED, VEC, KEEP, THREADS, CHUNKS>, dim3(grad_blocks(a.rows, a.cols, DTYPE)), dim3(grad_block<THREADS>()), smem, st, false,
+    e = launch_prio(k_q8_norm_grad<DTYPE, PACKED, VEC, KEEP, THREADS, CHUNKS>, dim3(grad_blocks(a.rows, a.cols, DTYPE, VEC)), dim3(grad_block<THREADS>()), smem, st, false,
                     0, false, true, a);
     return e == cudaSuccess ? NSML_OK : cuda_error();
   };
   using std::integral_constant;
-  constexpr int C = DTYPE == NSML_F32 ? 2 : 4;
-  const int threads = grad_threads(a.cols, DTYPE);
+  constexpr int C = grad_chunks(DTYPE, VEC), kLeast = 128 / (8 * C);  // 4, 8 or 16
+  const int threads = grad_threads(a.cols, DTYPE, VEC);
   if (threads == 1024 && a.cols > 8192 * C) return go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+  if (threads == kLeast) return go(integral_constant<int, kLeast>{}, integral_constant<int, C>{});
   switch (threads) {
-    case 4: if constexpr (C == 4) return go(integral_constant<int, 4>{}, integral_constant<int, C>{});
-    case 8: if constexpr (C == 2) return go(integral_constant<int, 8>{}, integral_constant<int, C>{});
-    case 16: if constexpr (C == 4) return go(integral_constant<int, 16>{}, integral_constant<int, C>{});
+    case 16: if constexpr (kLeast == 4) return go(integral_constant<int, 16>{}, integral_constant<int, C>{});
     case 32: return go(integral_constant<int, 32>{}, integral_constant<int, C>{});
     case 64: return go(integral_constant<int, 64>{}, integral_constant<int, C>{});
     case 128: return go(integral_constant<int, 128>{}, integral_constant<int, C>{});
@@ -308,8 +340,13 @@ extern "C" {
 
 size_t nsml_q8_rms_norm_backward_workspace_bytes(int64_t cols) {
   if (cols < 1 || cols > NSML_Q8_MAX_NORM_COLS) return 0;
-  const int f32 = grad_blocks(NSML_Q8_MAX_ROWS, cols, NSML_F32), bf16 = grad_blocks(NSML_Q8_MAX_ROWS, cols, NSML_BF16);
-  return align_up((size_t)(f32 > bf16 ? f32 : bf16) * (size_t)cols * 4, 256);
+  int most = 0;
+  for (const int dtype : {NSML_F32, NSML_BF16})
+    for (const bool vec : {false, true}) {
+      const int blocks = grad_blocks(NSML_Q8_MAX_ROWS, cols, dtype, vec);
+      most = blocks > most ? blocks : most;
+    }
+  return align_up((size_t)most * (size_t)cols * 4, 256);
 }
 
 int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64_t lddh, const void* h, int64_t ldh,
@@ -331,14 +368,14 @@ int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64
     if (workspace_bytes < nsml_q8_rms_norm_backward_workspace_bytes(cols)) return NSML_ERR_CAPACITY;
   }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool vec = cols % 8 == 0 && rows16(dy, ldy, dtype) && rows16(dx, lddx, dtype) && aligned(weight, 16) &&
+                   (dh == nullptr || rows16(dh, lddh, dtype)) && (h == nullptr || rows16(h, ldh, dtype));
   if (rows > 0) {
     NormGradArgs a = {};
     a.dy = dy; a.dh = dh; a.h = h; a.codes = codes; a.scales = scales; a.rstd = rstd; a.weight = weight; a.dx = dx;
     a.partial = dweight != nullptr ? static_cast<float*>(workspace) : nullptr;
     a.rows = rows; a.cols = (int)cols; a.ldy = ldy; a.lddh = lddh; a.ldh = ldh; a.ldq = ldq; a.lddx = lddx;
     a.weight_bf16 = weight_dtype == NSML_BF16;
-    const bool vec = cols % 8 == 0 && rows16(dy, ldy, dtype) && rows16(dx, lddx, dtype) && aligned(weight, 16) &&
-                     (dh == nullptr || rows16(dh, lddh, dtype)) && (h == nullptr || rows16(h, ldh, dtype));
     const bool packed = codes != nullptr;
     const bool keep = weight_dtype == dtype;
     auto by_flags = [&](auto type) {
@@ -356,7 +393,7 @@ int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64
   if (dweight != nullptr) {
     LaunchScope scope(K_Q8_NORM_WEIGHT, st);
     const cudaError_t e = launch_prio(k_q8_norm_weight, dim3((unsigned int)((cols + 31) / 32)), dim3(1024), 0, st, false, 0, true, true,
-                                      static_cast<const float*>(workspace), grad_blocks(rows, cols, dtype), cols, dweight,
+                                      static_cast<const float*>(workspace), grad_blocks(rows, cols, dtype, vec), cols, dweight,
                                       dweight_dtype == NSML_BF16, zero_first != 0);
     if (e != cudaSuccess) return cuda_error();
   }

@@ -33,10 +33,10 @@ k_q8_pack(const typename Elem<DTYPE>::type* __restrict__ x, int64_t rows, int co
   const int64_t row = my_row<THREADS>();
   const int lane = my_lane<THREADS>(), end = row < rows ? cols : 0;  // (a row behind the last: nothing is read or written)
   const auto* from = x + row * ldx;
-  Raw8<DTYPE> r[kChunks];
+  Raw8<DTYPE, VEC> r[kChunks];
   float top = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kChunks; ++i) r[i].template load<VEC, THREADS>(from, lane, i, end);
+  for (int i = 0; i < kChunks; ++i) r[i].template load<THREADS>(from, lane, i, end);
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
     if (empty<VEC, THREADS>(i, cols)) break;
@@ -89,14 +89,16 @@ k_q8_unpack(const int8_t* __restrict__ codes, int64_t ldq, const float* __restri
   const float scale = scales[row];
   const int8_t* from = codes + row * ldq + first;
   auto* to = out + row * ldo + first;
-  uint2 q[kChunks];
+  RawCodes8<VEC> q[kChunks];
 #pragma unroll
-  for (int i = 0; i < kChunks; ++i) q[i] = load8_codes<VEC, THREADS>(from, lane, i, end);
+  for (int i = 0; i < kChunks; ++i) q[i].template load<THREADS>(from, lane, i, end);
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
     if (empty<VEC, THREADS>(i, end)) break;
     float v[8];
-    restore8_codes(q[i], scale, v);
+    q[i].numbers(v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], scale);
     store8<DTYPE, VEC, THREADS>(to, lane, i, end, v);
   }
 }
@@ -138,14 +140,14 @@ __global__ void __launch_bounds__(block_threads<THREADS>()) k_q8_norm(const Norm
   const int64_t row = my_row<THREADS>();
   const int end = row < a.rows ? a.cols : 0;
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-  Raw8<DTYPE> h[kChunks];
+  Raw8<DTYPE, VEC> h[kChunks];
 #pragma unroll
-  for (int i = 0; i < kChunks; ++i) h[i].template load<VEC, THREADS>(x, lane, i, end);
+  for (int i = 0; i < kChunks; ++i) h[i].template load<THREADS>(x, lane, i, end);
   if (a.residual != nullptr) {
     const T* r = static_cast<const T*>(a.residual) + row * a.ldr;
-    Raw8<DTYPE> w[kChunks];
+    Raw8<DTYPE, VEC> w[kChunks];
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) w[i].template load<VEC, THREADS>(r, lane, i, end);
+    for (int i = 0; i < kChunks; ++i) w[i].template load<THREADS>(r, lane, i, end);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (empty<VEC, THREADS>(i, a.cols)) break;
@@ -160,7 +162,7 @@ __global__ void __launch_bounds__(block_threads<THREADS>()) k_q8_norm(const Norm
   if (a.h != nullptr) {
     T* to = static_cast<T*>(a.h) + row * a.ldh;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) h[i].template store<VEC, THREADS>(to, lane, i, end);
+    for (int i = 0; i < kChunks; ++i) h[i].template store<THREADS>(to, lane, i, end);
   }
   float y[kChunks][8];
   double sums[4] = {0.0, 0.0, 0.0, 0.0};  // (chains a quarter as long)
