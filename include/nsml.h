@@ -469,6 +469,7 @@ int nsml_decompress_accumulate_host(const void* const* payloads_host, const size
 #define NSML_Q8_MAX_COLS 2147483632LL
 #define NSML_Q8_MAX_NORM_COLS 32768   /* widest row of the norm */
 #define NSML_Q8_MAX_DEPTH 131071      /* longest sum of nsml_q8_matmul: 128 * 128 * 131071 < 2^31 */
+#define NSML_Q8_MAX_GRAD_DEPTH 4194304LL /* longest sum of the products' gradients */
 #define NSML_Q8_MATMUL_WORKSPACE_BYTES 256 /* the products' workspace holds a status word only */
 
 /* Smallest row stride, in bytes, of codes with `cols` columns (0 if out of range). */
@@ -521,7 +522,9 @@ int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64
 /* nsml_q8_matmul -- product of activations a[m, k] and weights b[n, k], both q8:
  *   out[i, j] = (sum_t a[i, t] * b[j, t]) * a_scales[i] * b_scales[j]
  * The sum is exact (32-bit integers; k <= NSML_Q8_MAX_DEPTH), then two float32
- * multiplies and one rounding to dtype.  Any int8 codes and float32 scales. */
+ * multiplies and one rounding to dtype.  Any int8 codes and float32 scales.
+ * workspace   256-byte aligned, >= NSML_Q8_MATMUL_WORKSPACE_BYTES; one call at a
+ *             time uses it (also for the gradients below) */
 int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const int8_t* b, int64_t ldb, const float* b_scales,
                    int64_t m, int64_t n, int64_t k, void* out, int64_t ldo, int dtype, void* workspace,
                    size_t workspace_bytes, void* stream);
@@ -531,10 +534,15 @@ int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const in
  *   nsml_q8_matmul_grad_input    dx[m, k] = sum_j dy[i, j] * (b[j, t] * b_scales[j])
  *   nsml_q8_matmul_grad_weight   dw[n, k] = [dw +] sum_i dy[i, j] * (a[i, t] * a_scales[i])
  * code * scale enters the product as a bfloat16: exact for power-of-two scales
- * from 2^-126 to 2^119, rounded to nearest otherwise.  Sums are float32, each
- * output is rounded once (zero_first = 0: after one float32 add).  dw may be a
- * slice of a gradient bucket (aligned to its elements, any row stride >= k).
- * m = 0 leaves a sum of nothing: dw is zeroed, or left as it is. */
+ * from 2^-126 on, rounded to nearest otherwise.  Sums are float32 (on tensor
+ * cores, which cut off instead of rounding; float32 outputs are summed in pieces
+ * of 2048 products), each output is rounded once (zero_first = 0: after one
+ * float32 add; float32 outputs: after an add per piece).  dw may be a slice of a
+ * gradient bucket (aligned to its elements, any row stride >= k).  The sums' length
+ * (n, respectively m) is at most NSML_Q8_MAX_GRAD_DEPTH.  Outputs overlap no input.
+ * m = 0 leaves a sum of nothing: dw is zeroed, or left as it is.
+ * A bounded wait inside a product that runs out (two seconds) is reported as
+ * NSML_ERR_TIMEOUT in the workspace's status word (nsml_last_status). */
 int nsml_q8_matmul_grad_input(const void* dy, int64_t ldy, const int8_t* b, int64_t ldb, const float* b_scales, int64_t m,
                               int64_t n, int64_t k, void* dx, int64_t lddx, int dtype, void* workspace,
                               size_t workspace_bytes, void* stream);

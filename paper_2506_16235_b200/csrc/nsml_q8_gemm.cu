@@ -15,7 +15,8 @@
 // too small to fill the GPU.
 //
 // The tensor cores cut float32 sums off instead of rounding them (measured: a relative error of 3e-10 per product of a sum),
-// so float32 results are summed in pieces of kPiece products, which are added with rounding.
+// so float32 results are summed in pieces of kPiece products, which are added with rounding: 4e-7 instead of 6e-6 for 16384
+// products.  A bfloat16 result of the pairs' form is one sum (at most 2^22 products: 1.3e-3, less than its rounding).
 #include <cuda.h>
 
 #include <mutex>
@@ -63,32 +64,31 @@ __device__ __forceinline__ unsigned long long now_ns() {
   asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
   return t;
 }
+// CLUSTER: arrivals of both blocks of a pair are waited for
+template <bool CLUSTER>
+__device__ __forceinline__ bool bar_try_at(uint32_t bar, uint32_t parity) {
+  if constexpr (!CLUSTER) return bar_try(bar, parity);
+  uint32_t done;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
 // false: the wait ran out (here or, as `failed` says, elsewhere in the block)
+template <bool CLUSTER>
 __device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile int* failed) {
   const unsigned long long from = now_ns();
   while (true) {
     for (int i = 0; i < 64; ++i)
-      if (bar_try(bar, parity)) return true;
+      if (bar_try_at<CLUSTER>(bar, parity)) return true;
     if (*failed != 0 || now_ns() - from > kWaitNs) {
       *failed = 1;
       return false;
     }
   }
 }
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
-  if (bar_try(bar, parity)) return true;
-  return bar_wait_slow(bar, parity, failed);
-}
-
-// waits for arrivals of both blocks of a pair
-__device__ __forceinline__ bool bar_try_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}"
-               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-  return done != 0;
-}
-__device__ __forceinline__ bool bar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* failed) {
-  return bar_wait(bar, parity, failed) && bar_try_cluster(bar, parity);  // (the phase is over: the second look orders memory)
+  return bar_try_at<CLUSTER>(bar, parity) || bar_wait_slow<CLUSTER>(bar, parity, failed);
 }
 __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {  // the same place in another block of the cluster
   uint32_t r;
@@ -438,14 +438,14 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
       for (int64_t t = first; ok && t < tiles; t += stride) {
         for (int piece = from; ok && piece < to; piece += g.piece, ++unit) {
           const uint32_t buffer = unit & 1, acc = tmem + buffer * S::kTile;
-          if (!(ok = bar_wait_cluster(acc_empty + 8 * buffer, ((unit >> 1) + 1) & 1, &failed))) break;
+          if (!(ok = bar_wait<PAIR>(acc_empty + 8 * buffer, ((unit >> 1) + 1) & 1, &failed))) break;
           tc_fence_after();
           const int end = min(to, piece + g.piece);
           for (int k = piece; k < end; ++k, ++it) {
             const uint32_t s = it % S::kStages, at = ring + s * S::kStage, w = it % S::kWides, wide = ring + S::kWideAt + w * S::kWide;
             if (!(ok = bar_wait(full + 8 * s, (it / S::kStages) & 1, &failed))) break;
             if constexpr (MODE != kForward)
-              if (!(ok = bar_wait_cluster(wide_full + 8 * w, (it / S::kWides) & 1, &failed))) break;
+              if (!(ok = bar_wait<PAIR>(wide_full + 8 * w, (it / S::kWides) & 1, &failed))) break;
             tc_fence_after();
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -763,6 +763,7 @@ template <int MODE>
 static int launch_gemm(const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_scales, GemmArgs g, const GemmDevice& dev, cudaStream_t st) {
   const int form = choose_form(g, dev, MODE == kForward ? 0.30 : 0.36);
   const int tile = form == 0 ? 256 : 128;
+  if (MODE == kForward || (form == 0 && g.bf16)) g.piece = g.steps;  // (integers are exact)
   g.tiles_m = up(g.rows, tile);
   g.tiles_n = up(g.cols, tile);
   const int64_t tiles = g.tiles_m * g.tiles_n;
@@ -832,7 +833,6 @@ int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const in
   g.col_scale = b_scales;
   g.depth = k;
   g.steps = (int)((k + 127) / 128);
-  g.piece = g.steps;
   CUtensorMap map_a, map_b;
   if (!tensor_map(&map_a, a, true, m, k, lda, 128, 128, true) || !tensor_map(&map_b, b, true, n, k, ldb, 128, 128, true)) return NSML_ERR_CUDA;
   return launch_gemm<kForward>(map_a, map_b, map_b, g, *dev, static_cast<cudaStream_t>(stream));
@@ -840,7 +840,7 @@ int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const in
 
 int nsml_q8_matmul_grad_input(const void* dy, int64_t ldy, const int8_t* b, int64_t ldb, const float* b_scales, int64_t m, int64_t n, int64_t k,
                               void* dx, int64_t lddx, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!valid_size(m) || !valid_size(n) || !valid_size(k) || n < 1 || k < 1) return NSML_ERR_ARG;
+  if (!valid_size(m) || !valid_size(n) || !valid_size(k) || n < 1 || k < 1 || n > NSML_Q8_MAX_GRAD_DEPTH) return NSML_ERR_ARG;
   if (m == 0) return NSML_OK;
   if (!valid_gradient(dy, m, n, ldy) || !valid_operand(b, n, k, ldb) || b_scales == nullptr || !aligned(b_scales, 4)) return NSML_ERR_ARG;
   int rc = check_out(dx, m, k, lddx, dtype, workspace, workspace_bytes);
@@ -850,7 +850,7 @@ int nsml_q8_matmul_grad_input(const void* dy, int64_t ldy, const int8_t* b, int6
   GemmArgs g = result(dx, m, k, lddx, dtype, false, workspace);
   g.depth = n;
   g.steps = (int)((n + 63) / 64);
-  g.piece = g.bf16 ? g.steps : kStepsPerPiece;
+  g.piece = kStepsPerPiece;
   CUtensorMap map_a, map_b, map_scales;
   if (!scales_map(&map_scales, b_scales, n, &g.scale_shift) || !tensor_map(&map_a, dy, false, m, n, ldy, 64, 128, true) || !tensor_map(&map_b, b, true, n, k, ldb, 128, 64, false)) return NSML_ERR_CUDA;
   return launch_gemm<kGradInput>(map_a, map_b, map_scales, g, *dev, static_cast<cudaStream_t>(stream));
@@ -858,7 +858,7 @@ int nsml_q8_matmul_grad_input(const void* dy, int64_t ldy, const int8_t* b, int6
 
 int nsml_q8_matmul_grad_weight(const void* dy, int64_t ldy, const int8_t* a, int64_t lda, const float* a_scales, int64_t m, int64_t n, int64_t k,
                                void* dw, int64_t lddw, int dtype, int zero_first, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!valid_size(m) || !valid_size(n) || !valid_size(k) || n < 1 || k < 1) return NSML_ERR_ARG;
+  if (!valid_size(m) || !valid_size(n) || !valid_size(k) || n < 1 || k < 1 || m > NSML_Q8_MAX_GRAD_DEPTH) return NSML_ERR_ARG;
   if (m > 0 && (!valid_gradient(dy, m, n, ldy) || !valid_operand(a, m, k, lda) || a_scales == nullptr || !aligned(a_scales, 4))) return NSML_ERR_ARG;
   int rc = check_out(dw, n, k, lddw, dtype, workspace, workspace_bytes);
   if (rc != NSML_OK) return rc;
@@ -874,7 +874,7 @@ int nsml_q8_matmul_grad_weight(const void* dy, int64_t ldy, const int8_t* a, int
   GemmArgs g = result(dw, n, k, lddw, dtype, zero_first == 0, workspace);
   g.depth = m;
   g.steps = (int)((m + 63) / 64);
-  g.piece = g.bf16 ? g.steps : kStepsPerPiece;
+  g.piece = kStepsPerPiece;
   CUtensorMap map_a, map_b, map_scales;
   if (!scales_map(&map_scales, a_scales, m, &g.scale_shift) || !tensor_map(&map_a, dy, false, m, n, ldy, 64, 64, true) || !tensor_map(&map_b, a, true, m, k, lda, 128, 64, false)) return NSML_ERR_CUDA;
   return launch_gemm<kGradWeight>(map_a, map_b, map_scales, g, *dev, st);

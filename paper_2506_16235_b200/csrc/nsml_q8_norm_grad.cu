@@ -1,4 +1,5 @@
 // Gradient of the RMS norm with an 8-bit output (nsml_q8.cuh).  It streams: its floor is the bytes of its arguments.
+#include <atomic>
 #include <type_traits>
 
 #include "nsml_launch.h"
@@ -305,10 +306,17 @@ static int norm_grad_rows(const NormGradArgs& a, cudaStream_t st) {
   auto go = [&](auto threads, auto chunks) {
     constexpr int THREADS = threads, CHUNKS = chunks;
     constexpr size_t smem = GradStage<DTYPE, VEC, THREADS, CHUNKS>::kSmem;
-    // (more than 48 KB has to be allowed; a setting of the function on the current device, not a call to it)
-    cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(k_q8_norm_grad<DTYPE, PACKED, VEC, KEEP, THREADS, CHUNKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)
-                                     : cudaSuccess;
-    if (e != cudaSuccess) return cuda_error();
+    cudaError_t e = cudaSuccess;
+    if constexpr (smem > 40 * 1024) {  // more than 48 KB have to be allowed, once per kernel and device
+      static std::atomic<unsigned long long> allowed{0};
+      int dev = 0;
+      if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cuda_error();
+      if ((allowed.load(std::memory_order_relaxed) >> dev & 1) == 0) {
+        e = cudaFuncSetAttribute(k_q8_norm_grad<DTYPE, PACKED, VEC, KEEP, THREADS, CHUNKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return cuda_error();
+        allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+      }
+    }
     LaunchScope scope(K_Q8_NORM_GRAD, st);
     e = launch_prio(k_q8_norm_grad<DTYPE, PACKED, VEC, KEEP, THREADS, CHUNKS>, dim3(grad_blocks(a.rows, a.cols, DTYPE, VEC)), dim3(grad_block<THREADS>()), smem, st, false,
                     0, false, true, a);

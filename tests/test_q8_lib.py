@@ -165,6 +165,7 @@ def test_products_refuse(at):
         for bad in (dict(dy=None), dict(dy=at + 8), dict(ldy=8), dict(ldy=12)):
             assert call(**bad) == ARG, (call.__name__, bad)
     assert forward(k=131072, lda=131072, ldb=131072) == ARG  # 128 * 128 * 131072 = 2^31
+    assert grad_input(n=4194305, ldy=4194312, ldb=32) == ARG == grad_weight(m=4194305)  # longest sums of the gradients
     assert forward(m=0, a=None, out=None) == nsml.NSML_OK == grad_input(m=0, dy=None, out=None)
 
 
