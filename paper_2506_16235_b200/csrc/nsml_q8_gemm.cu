@@ -391,6 +391,22 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
   const int64_t high = PAIR ? 16 : 32, stride = PAIR ? clusters : tiles;
   const int from = PAIR ? 0 : (int)((int64_t)g.steps * rank / blocks), to = PAIR ? g.steps : (int)((int64_t)g.steps * (rank + 1) / blocks);
 
+  // PAIR false: in the end a warp takes a row of the tile at a time, rows dealt out to the blocks.  Its scales are fetched now.
+  [[maybe_unused]] const int dealt = (int)blocks * (S::kThreads / 32);  // from a warp's row to its next one
+  [[maybe_unused]] int64_t tile_m = 0, col = 0;
+  [[maybe_unused]] float cs[4] = {}, my_scale = 0.0f;
+  if constexpr (!PAIR) {
+    int64_t n;
+    tile_at(first, high, g.tiles_m, g.tiles_n, tile_m, n);
+    col = n * 128 + 4 * lane;
+    if constexpr (MODE == kForward) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) cs[i] = col + i < g.cols ? g.col_scale[col + i] : 0.0f;
+      const int rr = rank + blocks * warp + lane * dealt;  // (lane i: the scale of the warp's i-th row)
+      if (rr < 128 && tile_m * 128 + rr < g.rows) my_scale = g.row_scale[tile_m * 128 + rr];
+    }
+  }
+
   if (warp == 0 || (MODE != kForward && warp == 3)) {
     if (elect_one()) {  // ---- loads: warp 0 what the tensor cores read, warp 3 codes
       uint32_t it = 0;
@@ -617,35 +633,28 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
   cluster_sync();  // PAIR: neither block's memory is used by the other any more.  Otherwise: every block's part is complete
   tc_fence_after();
   if (warp == 2) tmem_free<PAIR, S::kTmem>(tmem);
-  if constexpr (!PAIR) {  // a warp per row of the tile, rows dealt out to the blocks
-    const uint32_t parts = ring;
-    int64_t m, n;
-    tile_at(first, high, g.tiles_m, g.tiles_n, m, n);
-    const int64_t col = n * 128 + 4 * lane;
-    float cs[4];
-    if constexpr (MODE == kForward) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) cs[i] = col + i < g.cols ? g.col_scale[col + i] : 0.0f;
-    }
-    for (int rr = rank + blocks * warp; rr < 128 && m * 128 + rr < g.rows; rr += blocks * (S::kThreads / 32)) {
-      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      int sum[4] = {0, 0, 0, 0};
+  if constexpr (!PAIR) {
+    const int last = (int)min((int64_t)128, g.rows - tile_m * 128);
+    // (one row at a time: four at a time are more code, which is fetched for the first time here, and 1 us slower)
+#pragma unroll 1
+    for (int i = 0, rr = rank + blocks * warp; rr < last; ++i, rr += dealt) {
+      uint32_t sum[4] = {0, 0, 0, 0};
       for (uint32_t p = 0; p < blocks; ++p) {
         uint32_t x[4];
         asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
-                     : "r"(in_block(parts + (rr * S::kRow + 4 * lane) * 4, p)));
+                     : "r"(in_block(ring + (rr * S::kRow + 4 * lane) * 4, p)));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (MODE == kForward) sum[i] += (int)x[i];
-          else v[i] = p == 0 ? __uint_as_float(x[i]) : __fadd_rn(v[i], __uint_as_float(x[i]));
+        for (int j = 0; j < 4; ++j) {
+          if (MODE == kForward) sum[j] += x[j];
+          else sum[j] = p == 0 ? x[j] : __float_as_uint(__fadd_rn(__uint_as_float(sum[j]), __uint_as_float(x[j])));
         }
       }
-      if constexpr (MODE == kForward) {
-        const float rs = g.row_scale[m * 128 + rr];
+      const float rs = __shfl_sync(0xFFFFFFFFu, my_scale, i);
+      float v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __fmul_rn(__fmul_rn((float)sum[i], rs), cs[i]);
-      }
-      put<4>(g, m * 128 + rr, col, g.add, v);
+      for (int j = 0; j < 4; ++j)
+        v[j] = MODE == kForward ? __fmul_rn(__fmul_rn((float)(int)sum[j], rs), cs[j]) : __uint_as_float(sum[j]);
+      put<4>(g, tile_m * 128 + rr, col, g.add, v);
     }
     cluster_sync();  // no block leaves while another reads its part
   }
