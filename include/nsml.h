@@ -14,6 +14,9 @@
  *                                       (Section 4.2 Step 3; AllGather pattern
  *                                       of Section 5.3)
  *
+ * and what makes the gradients before that, in 8 bits (nsml_q8_*): activations
+ * stored and restored, the RMS norm, the matrix product, and their gradients.
+ *
  * `ratio` is the KEPT fraction, as in the paper (1 = send everything).
  *
  * Conventions

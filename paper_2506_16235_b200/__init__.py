@@ -11,6 +11,13 @@ if the library has not been built.
     ratio = ctrl.select_ratio(last_bytes, last_seconds, dense_bytes)
     payload = nsml.nsml_compress(grad, ratio, bits=8)
     nsml.nsml_decompress_accumulate([payload, ...], dense, zero_first=True)
+
+Training in 8 bits (codes are int8 [rows, cols] tensors whose rows start on
+16-byte boundaries, scales float32 [rows]); dp.NormLinear puts them together:
+    codes, scales, rstd, h = nsml.nsml_q8_rms_norm(x, norm_weight, residual=r)
+    w, w_scales = nsml.nsml_q8_pack(weight)
+    y = nsml.nsml_q8_matmul(codes, scales, w, w_scales)
+    nsml.nsml_q8_matmul_grad_weight(dy, codes, scales, dw=bucket_slice)
 """
 from __future__ import annotations
 

@@ -29,7 +29,8 @@ struct NormGradArgs {
 // rows next to each other, and every so many-th row after them.  A thread's chunks of the next row are copied to its own places
 // in shared memory meanwhile (asynchronous copies: no registers, and no barrier, since nobody else reads them); it reads them
 // there twice and keeps its columns' part of dweight in registers.  The block's rows add theirs up in the end, so that the
-// sum's order depends on the sizes alone.
+// sum's order depends on the sizes alone.  16384 x 2048 bfloat16, rows in 8 bits and dh: 41 us with the weight's sum behind it
+// (235 MB, 5.7 TB/s); from bfloat16 rows without dh 36 us.  Rows off 16-byte boundaries: 16383 x 2047 67 us.
 constexpr int kGradBlock = 256;
 
 template <int THREADS>
@@ -260,7 +261,8 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
   }
 }
 
-// dweight (+)= sum of the blocks' parts, in their order
+// dweight (+)= sum of the blocks' parts, in their order.  A block has 32 columns, its warps every 32nd part: dependent reads
+// bound it, 4-5 us behind the kernel above for 296 parts.
 __global__ void __launch_bounds__(1024) k_q8_norm_weight(const float* __restrict__ partial, int parts, int64_t cols, void* dweight,
                                                         bool bf16, bool zero_first) {
   __shared__ float sums[32][33];
