@@ -210,7 +210,7 @@ struct GemmArgs {
   int piece;                 // blocks per piece of the sum
   void* out;
   int64_t ldo;
-  bool bf16, add, vec;       // vec: rows of the result start on 16-byte boundaries
+  bool bf16, add, vec, even; // vec: rows of the result start on 16-byte boundaries; even: on 4-byte ones
   const float* row_scale;    // kForward
   const float* col_scale;    // kForward
   int scale_shift;           // gradients: where the first scale is in the tensor map's first four
@@ -223,7 +223,7 @@ template <int MODE, bool PAIR>
 struct Shape {
   static constexpr int kTile = PAIR ? 256 : 128;
   static constexpr int kStage = MODE == kForward ? 2 * 128 * 128 : 128 * 128;  // bytes of a stage: the first operand; kForward: both
-  static constexpr int kStages = 6;
+  static constexpr int kStages = PAIR && MODE == kForward ? 5 : 6;
   // gradients: the second operand's codes with the scales of their rows (68 of them, so that 64 start anywhere), and restored
   static constexpr int kCode = MODE == kForward ? 0 : 128 * 64 + 384;
   static constexpr int kCodes = 4;
@@ -235,10 +235,11 @@ struct Shape {
   // every turn meets every phase of its slots of the rings (a wait tells a phase from the next one only, not from the one after)
   static_assert(kCodes % kTurns == 0 && kWides % kTurns == 0, "");
   static constexpr int kWideAt = kStages * kStage, kCodeAt = kWideAt + kWides * kWide, kRings = kCodeAt + kCodes * kCode;
-  static constexpr int kThreads = MODE == kForward ? 256 : 512;
+  static constexpr int kOutWarps = MODE == kForward ? 8 : 4;  // warps that take results out; a quarter of the rows, and part of the columns, each
+  static constexpr int kThreads = MODE == kForward ? 128 + 32 * kOutWarps : 512;
   // PAIR: staging of results on their way out.  Otherwise a block's part of the results takes the rings' place at the end,
   // rows of kRow floats.
-  static constexpr int kOut = PAIR ? 4 * (32 * 128 + (MODE == kForward ? 256 * 4 : 0)) : 0;
+  static constexpr int kOut = PAIR ? kOutWarps * (32 * 128 + (MODE == kForward ? 128 * 4 : 0)) : 0;
   static constexpr int kRow = 132;
   static_assert(PAIR || 128 * kRow * 4 <= kRings, "");
   // two accumulators, one is read while the other is filled; PAIR false: and the sum of the pieces so far
@@ -277,65 +278,79 @@ __device__ __forceinline__ uint4 restore8(uint32_t w0, uint32_t w1, float scale)
 }
 
 // ---- results out ---------------------------------------------------------------------------------------------------------
-// COUNT consecutive results of a row, in float32, to their place: `add`: on top of what is there, with one addition.
-template <int COUNT>
-__device__ __forceinline__ void put(const GemmArgs& g, int64_t row, int64_t col, bool add, const float (&v)[COUNT]) {
+// One result, in float32, to its place; g.add or `add`: on top of what is there, with one addition.
+__device__ __forceinline__ void put1(const GemmArgs& g, int64_t row, int64_t col, bool add, float v) {
   if (row >= g.rows || col >= g.cols) return;
-  const bool whole = g.vec && col + COUNT <= g.cols;
   if (g.bf16) {
     __nv_bfloat16* to = static_cast<__nv_bfloat16*>(g.out) + row * g.ldo + col;
-    if (whole) {
-      uint32_t w[COUNT / 2];
-#pragma unroll
-      for (int i = 0; i < COUNT / 2; ++i) {
-        float a = v[2 * i], b = v[2 * i + 1];
-        if (add) {
-          float p, q;
-          unpack2(reinterpret_cast<const uint32_t*>(to)[i], p, q);
-          a = __fadd_rn(a, p);
-          b = __fadd_rn(b, q);
-        }
-        w[i] = pack2(a, b);
-      }
-      if constexpr (COUNT == 4) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
-      else *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i)
-      if (col + i < g.cols) to[i] = __float2bfloat16_rn(add ? __fadd_rn(v[i], (float)to[i]) : v[i]);
-    return;
+    *to = __float2bfloat16_rn(add ? __fadd_rn(v, (float)*to) : v);
+  } else {
+    float* to = static_cast<float*>(g.out) + row * g.ldo + col;
+    *to = add ? __fadd_rn(v, *to) : v;
   }
-  float* to = static_cast<float*>(g.out) + row * g.ldo + col;
-  if (whole) {
-#pragma unroll
-    for (int i = 0; i < COUNT; i += 4) {
-      float4 w = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-      if (add) {
-        const float4 o = *reinterpret_cast<const float4*>(to + i);
-        w = make_float4(__fadd_rn(w.x, o.x), __fadd_rn(w.y, o.y), __fadd_rn(w.z, o.z), __fadd_rn(w.w, o.w));
-      }
-      *reinterpret_cast<float4*>(to + i) = w;
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < COUNT; ++i)
-    if (col + i < g.cols) to[i] = add ? __fadd_rn(v[i], to[i]) : v[i];
 }
 
-// Eight results that are bfloat16 already (nothing is added to them).
-__device__ __forceinline__ void put_bf16(const GemmArgs& g, int64_t row, int64_t col, uint4 w) {
+// Four consecutive ones; the rows start on 16-byte boundaries (g.vec).
+__device__ __forceinline__ void put4(const GemmArgs& g, int64_t row, int64_t col, bool add, const float (&v)[4]) {
   if (row >= g.rows || col >= g.cols) return;
-  __nv_bfloat16* to = static_cast<__nv_bfloat16*>(g.out) + row * g.ldo + col;
-  if (g.vec && col + 8 <= g.cols) {
-    *reinterpret_cast<uint4*>(to) = w;
+  if (col + 4 > g.cols) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put1(g, row, col + i, add, v[i]);
     return;
   }
-  const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (col + i < g.cols) reinterpret_cast<uint16_t*>(to)[i] = (uint16_t)(words[i / 2] >> (16 * (i & 1)));
+  float4 o;
+  if (g.bf16) {
+    uint2* to = reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(g.out) + row * g.ldo + col);
+    if (add) {
+      const uint2 w = *to;
+      unpack2(w.x, o.x, o.y);
+      unpack2(w.y, o.z, o.w);
+      *to = make_uint2(pack2(__fadd_rn(v[0], o.x), __fadd_rn(v[1], o.y)), pack2(__fadd_rn(v[2], o.z), __fadd_rn(v[3], o.w)));
+    } else {
+      *to = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+    }
+  } else {
+    float4* to = reinterpret_cast<float4*>(static_cast<float*>(g.out) + row * g.ldo + col);
+    if (add) {
+      o = *to;
+      *to = make_float4(__fadd_rn(v[0], o.x), __fadd_rn(v[1], o.y), __fadd_rn(v[2], o.z), __fadd_rn(v[3], o.w));
+    } else {
+      *to = make_float4(v[0], v[1], v[2], v[3]);
+    }
+  }
+}
+
+// The words of 32 rows of 128 bytes that are staged in 16-byte pieces, swizzled: word `lane` of every row below `last`.
+template <class Put>
+__device__ __forceinline__ void each_row(const unsigned char* stage, int lane, int64_t last, Put put) {
+#pragma unroll 8
+  for (int rr = 0; rr < 32; ++rr) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(stage + rr * 128 + (((lane >> 2) ^ (rr & 7)) << 4) + 4 * (lane & 3));
+    if (rr < last) put(rr, w);
+  }
+}
+
+// Eight or two that are bfloat16 already (nothing is added to them); eight: g.vec.
+__device__ __forceinline__ void put_bf16(const GemmArgs& g, int64_t row, int64_t col, uint32_t pair) {
+  if (row >= g.rows || col >= g.cols) return;
+  uint16_t* to = static_cast<uint16_t*>(g.out) + row * g.ldo + col;
+  if (g.even && col + 2 <= g.cols) {
+    *reinterpret_cast<uint32_t*>(to) = pair;
+    return;
+  }
+  to[0] = (uint16_t)pair;
+  if (col + 1 < g.cols) to[1] = (uint16_t)(pair >> 16);
+}
+__device__ __forceinline__ void put_bf16(const GemmArgs& g, int64_t row, int64_t col, uint4 w) {
+  if (row >= g.rows || col >= g.cols) return;
+  if (col + 8 <= g.cols) {
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(g.out) + row * g.ldo + col) = w;
+    return;
+  }
+  put_bf16(g, row, col, w.x);
+  put_bf16(g, row, col + 2, w.y);
+  put_bf16(g, row, col + 4, w.z);
+  put_bf16(g, row, col + 6, w.w);
 }
 
 template <int MODE, bool PAIR>
@@ -373,7 +388,7 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(acc_full + 8 * i, 1);
-      bar_init(acc_empty + 8 * i, PAIR ? 8 : 4);
+      bar_init(acc_empty + 8 * i, PAIR ? 2 * S::kOutWarps : S::kOutWarps);
     }
     failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -484,8 +499,10 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
       }
     }
     __syncwarp();
-  } else if (warp >= 4 && warp < 8) {  // ---- results
-    const int quarter = warp - 4;
+  } else if (warp >= 4 && warp < 4 + S::kOutWarps) {  // ---- results
+    const int quarter = warp & 3;  // (a warp reaches the rows of TMEM that its number says)
+    constexpr int kChunks = S::kTile / 32 * 4 / S::kOutWarps;  // of 32 columns
+    const int first_chunk = (warp - 4) / 4 * kChunks;
     unsigned char* const out = ring_ptr + S::kRings;
     uint32_t unit = 0;
     bool ok = true;
@@ -505,21 +522,21 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
           }
         };
         if constexpr (PAIR) {
-          unsigned char* const stage = out + quarter * 4096;  // 32 rows of 128 bytes, pieces of 16 swizzled
-          float* const scales = reinterpret_cast<float*>(out + 4 * 4096) + quarter * 256;
-          const int64_t row0 = m * 256 + rank * 128 + quarter * 32, col0 = n * 256;
+          unsigned char* const stage = out + (warp - 4) * 4096;  // 32 rows of 128 bytes, pieces of 16 swizzled
+          float* const scales = reinterpret_cast<float*>(out + S::kOutWarps * 4096) + (warp - 4) * 128;
+          const int64_t row0 = m * 256 + rank * 128 + quarter * 32, col0 = n * 256 + first_chunk * 32;
           const bool add = g.add || piece > from, packed = g.bf16 && !add;
           float rs = 0.0f;
           if constexpr (MODE == kForward) {
             rs = row0 + lane < g.rows ? g.row_scale[row0 + lane] : 0.0f;
-            for (int i = lane; i < 256; i += 32) scales[i] = col0 + i < g.cols ? g.col_scale[col0 + i] : 0.0f;
+            for (int i = lane; i < 32 * kChunks; i += 32) scales[i] = col0 + i < g.cols ? g.col_scale[col0 + i] : 0.0f;
             __syncwarp();
           }
 #pragma unroll 1
-          for (int c = 0; c < 8; ++c) {
+          for (int c = 0; c < kChunks; ++c) {
             uint32_t r[32];
-            tmem_load32(acc + c * 32, r);
-            if (c == 7) release();
+            tmem_load32(acc + (first_chunk + c) * 32, r);
+            if (c == kChunks - 1) release();
             if constexpr (MODE == kForward) {
 #pragma unroll
               for (int j = 0; j < 32; j += 4) {
@@ -548,15 +565,43 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                 *reinterpret_cast<uint4*>(line + ((j ^ (lane & 7)) << 4)) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
             }
             __syncwarp();
+            if (g.vec) {  // 16 bytes per lane, four rows at a time
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int rr = 4 * i + (lane >> 3), j = lane & 7;
-              const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
-              if (packed) {
-                put_bf16(g, row0 + rr, col0 + (c >> 1) * 64 + 8 * j, w);
+              for (int i = 0; i < 8; ++i) {
+                const int rr = 4 * i + (lane >> 3), j = lane & 7;
+                const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
+                if (packed) {
+                  put_bf16(g, row0 + rr, col0 + (c >> 1) * 64 + 8 * j, w);
+                } else {
+                  const float v[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
+                  put4(g, row0 + rr, col0 + c * 32 + 4 * j, add, v);
+                }
+              }
+            } else if (packed) {  // 4 bytes per lane, a row at a time: stores next to each other wherever the row starts
+              const int64_t col = col0 + (c >> 1) * 64 + 2 * lane;
+              uint16_t* const to = static_cast<uint16_t*>(g.out) + row0 * g.ldo + col;
+              auto rows = [&](auto put) { each_row(stage, lane, col < g.cols ? g.rows - row0 : 0, [&](int rr, uint32_t w) { put(to + rr * g.ldo, w); }); };
+              if (g.even && col + 2 <= g.cols) {
+                rows([&](uint16_t* at, uint32_t w) { *reinterpret_cast<uint32_t*>(at) = w; });
               } else {
-                const float v[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
-                put<4>(g, row0 + rr, col0 + c * 32 + 4 * j, add, v);
+                const bool two = col + 1 < g.cols;
+                rows([&](uint16_t* at, uint32_t w) {
+                  at[0] = (uint16_t)w;
+                  if (two) at[1] = (uint16_t)(w >> 16);
+                });
+              }
+            } else if (MODE == kForward && !g.bf16) {  // the same: 21183 x 7026 from a sum of 64 314 -> 273 us
+              const int64_t col = col0 + c * 32 + lane;
+              uint32_t* const to = static_cast<uint32_t*>(g.out) + row0 * g.ldo + col;
+              each_row(stage, lane, col < g.cols ? g.rows - row0 : 0, [&](int rr, uint32_t w) { to[rr * g.ldo] = w; });
+            } else {  // (by the gradients' four warps a row at a time takes half as long again: 2047 x 2047 from 2049 34 us instead of 25)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int rr = 4 * i + (lane >> 3), j = lane & 7;
+                const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
+                const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) put1(g, row0 + rr, col0 + c * 32 + 4 * j + e, add, __uint_as_float(v[e]));
               }
             }
             __syncwarp();
@@ -565,10 +610,10 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
           const bool last = piece + g.piece >= to;
           float* const line = reinterpret_cast<float*>(ring_ptr) + (quarter * 32 + lane) * S::kRow;
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
+          for (int c = first_chunk; c < first_chunk + kChunks; ++c) {
             uint32_t r[32];
             tmem_load32(acc + c * 32, r);
-            if (c == 3) release();
+            if (c == first_chunk + kChunks - 1) release();
             const uint32_t sum = tmem + S::kSum + ((uint32_t)quarter << 21) + c * 32;
             if (piece > from) {  // (never integers)
               uint32_t o[32];
@@ -661,7 +706,12 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         v[j] = MODE == kForward ? __fmul_rn(__fmul_rn((float)(int)sum[j], rs), cs[j]) : __uint_as_float(sum[j]);
-      put<4>(g, tile_m * 128 + rr, col, g.add, v);
+      if (g.vec) {
+        put4(g, tile_m * 128 + rr, col, g.add, v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) put1(g, tile_m * 128 + rr, col + j, g.add, v[j]);
+      }
     }
     cluster_sync();  // no block leaves while another reads its part
   }
@@ -818,6 +868,7 @@ static GemmArgs result(void* out, int64_t rows, int64_t cols, int64_t ldo, int d
   g.ldo = ldo;
   g.bf16 = dtype == NSML_BF16;
   g.add = add;
+  g.even = aligned(out, 4) && (rows <= 1 || !g.bf16 || ldo % 2 == 0);
   g.vec = aligned(out, 16) && (rows <= 1 || ldo % (g.bf16 ? 8 : 4) == 0);
   g.status = static_cast<int*>(workspace);
   return g;
