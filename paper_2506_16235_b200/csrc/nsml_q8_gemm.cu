@@ -223,7 +223,7 @@ template <int MODE, bool PAIR>
 struct Shape {
   static constexpr int kTile = PAIR ? 256 : 128;
   static constexpr int kStage = MODE == kForward ? 2 * 128 * 128 : 128 * 128;  // bytes of a stage: the first operand; kForward: both
-  static constexpr int kStages = PAIR && MODE == kForward ? 5 : 6;
+  static constexpr int kStages = PAIR ? 5 : 6;
   // gradients: the second operand's codes with the scales of their rows (68 of them, so that 64 start anywhere), and restored
   static constexpr int kCode = MODE == kForward ? 0 : 128 * 64 + 384;
   static constexpr int kCodes = 4;
@@ -235,8 +235,8 @@ struct Shape {
   // every turn meets every phase of its slots of the rings (a wait tells a phase from the next one only, not from the one after)
   static_assert(kCodes % kTurns == 0 && kWides % kTurns == 0, "");
   static constexpr int kWideAt = kStages * kStage, kCodeAt = kWideAt + kWides * kWide, kRings = kCodeAt + kCodes * kCode;
-  static constexpr int kOutWarps = MODE == kForward ? 8 : 4;  // warps that take results out; a quarter of the rows, and part of the columns, each
-  static constexpr int kThreads = MODE == kForward ? 128 + 32 * kOutWarps : 512;
+  static constexpr int kOutWarps = 8;  // warps that take results out: a quarter of the rows and half of the columns each
+  static constexpr int kFirstRestorer = 4 + kOutWarps, kThreads = 32 * kFirstRestorer + (MODE == kForward ? 0 : 256);
   // PAIR: staging of results on their way out.  Otherwise a block's part of the results takes the rings' place at the end,
   // rows of kRow floats.
   static constexpr int kOut = PAIR ? kOutWarps * (32 * 128 + (MODE == kForward ? 128 * 4 : 0)) : 0;
@@ -320,37 +320,15 @@ __device__ __forceinline__ void put4(const GemmArgs& g, int64_t row, int64_t col
   }
 }
 
-// The words of 32 rows of 128 bytes that are staged in 16-byte pieces, swizzled: word `lane` of every row below `last`.
+// The words of 32 rows of 128 bytes that are staged in 16-byte pieces, swizzled: word `lane` of every row below `last`, and where
+// it goes.
 template <class Put>
-__device__ __forceinline__ void each_row(const unsigned char* stage, int lane, int64_t last, Put put) {
+__device__ __forceinline__ void each_row(const unsigned char* stage, int lane, int last, unsigned char* to, int64_t pitch, Put put) {
 #pragma unroll 8
-  for (int rr = 0; rr < 32; ++rr) {
+  for (int rr = 0; rr < 32; ++rr, to += pitch) {
     const uint32_t w = *reinterpret_cast<const uint32_t*>(stage + rr * 128 + (((lane >> 2) ^ (rr & 7)) << 4) + 4 * (lane & 3));
-    if (rr < last) put(rr, w);
+    if (rr < last) put(to, w);
   }
-}
-
-// Eight or two that are bfloat16 already (nothing is added to them); eight: g.vec.
-__device__ __forceinline__ void put_bf16(const GemmArgs& g, int64_t row, int64_t col, uint32_t pair) {
-  if (row >= g.rows || col >= g.cols) return;
-  uint16_t* to = static_cast<uint16_t*>(g.out) + row * g.ldo + col;
-  if (g.even && col + 2 <= g.cols) {
-    *reinterpret_cast<uint32_t*>(to) = pair;
-    return;
-  }
-  to[0] = (uint16_t)pair;
-  if (col + 1 < g.cols) to[1] = (uint16_t)(pair >> 16);
-}
-__device__ __forceinline__ void put_bf16(const GemmArgs& g, int64_t row, int64_t col, uint4 w) {
-  if (row >= g.rows || col >= g.cols) return;
-  if (col + 8 <= g.cols) {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(g.out) + row * g.ldo + col) = w;
-    return;
-  }
-  put_bf16(g, row, col, w.x);
-  put_bf16(g, row, col + 2, w.y);
-  put_bf16(g, row, col + 4, w.z);
-  put_bf16(g, row, col + 6, w.w);
 }
 
 template <int MODE, bool PAIR>
@@ -565,44 +543,48 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                 *reinterpret_cast<uint4*>(line + ((j ^ (lane & 7)) << 4)) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
             }
             __syncwarp();
-            if (g.vec) {  // 16 bytes per lane, four rows at a time
+            // (addresses are worked out once per block of 32 rows: with a bound and a product for every store the results of
+            // 13779 x 9100 from a sum of 9 took 151 us, those of 8192 x 8192 x 2048 a tenth of the whole)
+            const int size = g.bf16 ? 2 : 4, width = packed ? 64 : 32;
+            const int64_t block = col0 + (packed ? c >> 1 : c) * width;
+            unsigned char* const corner = static_cast<unsigned char*>(g.out) + (row0 * g.ldo + block) * size;
+            const int64_t pitch = g.ldo * size;
+            if (g.vec && row0 + 32 <= g.rows && block + width <= g.cols && (packed || !g.bf16)) {  // 16 bytes per lane, four rows at a time
+              unsigned char* to = corner + (lane >> 3) * pitch + 16 * (lane & 7);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
+              for (int i = 0; i < 8; ++i, to += 4 * pitch) {
                 const int rr = 4 * i + (lane >> 3), j = lane & 7;
-                const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
-                if (packed) {
-                  put_bf16(g, row0 + rr, col0 + (c >> 1) * 64 + 8 * j, w);
-                } else {
-                  const float v[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
-                  put4(g, row0 + rr, col0 + c * 32 + 4 * j, add, v);
+                uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
+                if (add) {
+                  const float4 o = *reinterpret_cast<const float4*>(to);
+                  w = make_uint4(__float_as_uint(__fadd_rn(__uint_as_float(w.x), o.x)), __float_as_uint(__fadd_rn(__uint_as_float(w.y), o.y)),
+                                 __float_as_uint(__fadd_rn(__uint_as_float(w.z), o.z)), __float_as_uint(__fadd_rn(__uint_as_float(w.w), o.w)));
                 }
+                *reinterpret_cast<uint4*>(to) = w;
               }
-            } else if (packed) {  // 4 bytes per lane, a row at a time: stores next to each other wherever the row starts
-              const int64_t col = col0 + (c >> 1) * 64 + 2 * lane;
-              uint16_t* const to = static_cast<uint16_t*>(g.out) + row0 * g.ldo + col;
-              auto rows = [&](auto put) { each_row(stage, lane, col < g.cols ? g.rows - row0 : 0, [&](int rr, uint32_t w) { put(to + rr * g.ldo, w); }); };
-              if (g.even && col + 2 <= g.cols) {
-                rows([&](uint16_t* at, uint32_t w) { *reinterpret_cast<uint32_t*>(at) = w; });
+            } else if (packed || (!g.bf16 && !add)) {  // 4 bytes per lane, a row at a time: stores next to each other wherever the row starts
+              const int64_t col = block + (packed ? 2 : 1) * lane;
+              const int last = col < g.cols ? (int)min((int64_t)32, g.rows - row0) : 0;
+              unsigned char* const to = corner + 4 * lane;
+              if (!packed || (g.even && col + 2 <= g.cols)) {
+                each_row(stage, lane, last, to, pitch, [](unsigned char* at, uint32_t w) { *reinterpret_cast<uint32_t*>(at) = w; });
               } else {
                 const bool two = col + 1 < g.cols;
-                rows([&](uint16_t* at, uint32_t w) {
-                  at[0] = (uint16_t)w;
-                  if (two) at[1] = (uint16_t)(w >> 16);
+                each_row(stage, lane, last, to, pitch, [&](unsigned char* at, uint32_t w) {
+                  reinterpret_cast<uint16_t*>(at)[0] = (uint16_t)w;
+                  if (two) reinterpret_cast<uint16_t*>(at)[1] = (uint16_t)(w >> 16);
                 });
               }
-            } else if (MODE == kForward && !g.bf16) {  // the same: 21183 x 7026 from a sum of 64 314 -> 273 us
-              const int64_t col = col0 + c * 32 + lane;
-              uint32_t* const to = static_cast<uint32_t*>(g.out) + row0 * g.ldo + col;
-              each_row(stage, lane, col < g.cols ? g.rows - row0 : 0, [&](int rr, uint32_t w) { to[rr * g.ldo] = w; });
-            } else {  // (by the gradients' four warps a row at a time takes half as long again: 2047 x 2047 from 2049 34 us instead of 25)
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int rr = 4 * i + (lane >> 3), j = lane & 7;
-                const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
-                const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) put1(g, row0 + rr, col0 + c * 32 + 4 * j + e, add, __uint_as_float(v[e]));
-              }
+            } else {  // on top of what is there, at the edges, off 16-byte boundaries or in bfloat16
+              each_row(stage, lane, block + lane < g.cols ? (int)min((int64_t)32, g.rows - row0) : 0, corner + size * lane, pitch, [&](unsigned char* at, uint32_t w) {
+                if (g.bf16) {
+                  __nv_bfloat16* const to = reinterpret_cast<__nv_bfloat16*>(at);
+                  *to = __float2bfloat16_rn(add ? __fadd_rn(__uint_as_float(w), (float)*to) : __uint_as_float(w));
+                } else {
+                  float* const to = reinterpret_cast<float*>(at);
+                  *to = __fadd_rn(__uint_as_float(w), *to);
+                }
+              });
             }
             __syncwarp();
           }
@@ -632,13 +614,13 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
         }
       }
     }
-  } else if (MODE != kForward && warp >= 8) {  // ---- codes to bfloat16: the warps take turns at the steps, kTurn of them at one
+  } else if (MODE != kForward && warp >= S::kFirstRestorer) {  // ---- codes to bfloat16: the warps take turns at the steps, kTurn of them at one
     if constexpr (MODE != kForward) {
       constexpr int kTurn = S::kTurn, kTurns = S::kTurns, kRows = 64 / kTurn;
-      const int sub = lane & 7, row = (warp - 8) % kTurn * kRows + (lane >> 3);
+      const int sub = lane & 7, row = (warp - S::kFirstRestorer) % kTurn * kRows + (lane >> 3);
       const int flip = sub >> 2, c0 = (sub & 3) * 2;  // lanes whose blocks of columns share banks write their halves in opposite order
       const int64_t mine = first < tiles ? (tiles - first + stride - 1) / stride : 0, total = mine * (to - from);
-      for (int64_t it = (warp - 8) / kTurn; it < total; it += kTurns) {
+      for (int64_t it = (warp - S::kFirstRestorer) / kTurn; it < total; it += kTurns) {
         const uint32_t s = (uint32_t)(it % S::kCodes), w = (uint32_t)(it % S::kWides);
         if (!bar_wait(codes_full + 8 * s, (uint32_t)(it / S::kCodes) & 1, &failed)) break;
         const unsigned char* codes = ring_ptr + S::kCodeAt + s * S::kCode;
