@@ -514,7 +514,10 @@ int nsml_q8_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t l
  *   dweight        cols elements of dweight_dtype (aligned to its elements: a
  *                  slice of a gradient bucket), or NULL; zero_first = 0 adds
  *   workspace      256-byte aligned, nsml_q8_rms_norm_backward_workspace_bytes(cols)
- *                  bytes; not needed (may be NULL) without dweight */
+ *                  bytes (no less for more columns); not needed (may be NULL)
+ *                  without dweight.  One call at a time uses it
+ * The float32 sums are of dy * h (with codes: of dy * code), which must not pass
+ * the type's range before rstd brings them back. */
 size_t nsml_q8_rms_norm_backward_workspace_bytes(int64_t cols);
 int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64_t lddh, const void* h, int64_t ldh,
                               const int8_t* codes, int64_t ldq, const float* scales, const float* rstd, int64_t rows,
@@ -524,8 +527,9 @@ int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64
 
 /* nsml_q8_matmul -- product of activations a[m, k] and weights b[n, k], both q8:
  *   out[i, j] = (sum_t a[i, t] * b[j, t]) * a_scales[i] * b_scales[j]
- * The sum is exact (32-bit integers; k <= NSML_Q8_MAX_DEPTH), then two float32
- * multiplies and one rounding to dtype.  Any int8 codes and float32 scales.
+ * The sum is exact (32-bit integers; k <= NSML_Q8_MAX_DEPTH), then converted to
+ * float32, multiplied twice in float32 and rounded to dtype.  Any int8 codes and
+ * float32 scales.  The output overlaps no input.
  * workspace   256-byte aligned, >= NSML_Q8_MATMUL_WORKSPACE_BYTES; one call at a
  *             time uses it (also for the gradients below) */
 int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const int8_t* b, int64_t ldb, const float* b_scales,

@@ -32,7 +32,7 @@ __device__ __forceinline__ float scale_of(uint32_t amax_bits, float* inv) {
 
 // Four codes of values times inv (exact: a power of two).  Adding 1.5 * 2^23 rounds to an integer, half to even, whose low
 // byte is the code.  clamp: products may round to 128 (a scale held at 2^121), or the row is not finite (inv is 0: codes 0).
-__device__ __forceinline__ bool needs_clamp(uint32_t amax_bits) { return amax_bits >= 0x7EFF0000u; }  // 127.5 * 2^121
+__device__ __forceinline__ bool needs_clamp(uint32_t amax_bits) { return amax_bits >= 0x7F7F0000u; }  // 127.5 * 2^121
 template <bool CLAMP>
 __device__ __forceinline__ uint32_t code_bits(float v, float inv) {
   if constexpr (CLAMP) {

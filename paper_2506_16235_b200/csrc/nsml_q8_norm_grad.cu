@@ -264,10 +264,11 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
 // dweight (+)= sum of the blocks' parts, in their order.  A block has 32 columns, its warps every 32nd part: dependent reads
 // bound it, 4-5 us behind the kernel above for 296 parts.
 __global__ void __launch_bounds__(1024) k_q8_norm_weight(const float* __restrict__ partial, int parts, int64_t cols, void* dweight,
-                                                        bool bf16, bool zero_first) {
+                                                        bool bf16, bool zero_first, int* status) {
   __shared__ float sums[32][33];
   pdl_wait();
   pdl_launch_dependents();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *status = NSML_OK;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t c = (int64_t)blockIdx.x * 32 + lane;
   float s = 0.0f;
@@ -290,6 +291,8 @@ __global__ void __launch_bounds__(1024) k_q8_norm_weight(const float* __restrict
 
 // The gradient of the norm: chunks per thread, threads per row, and blocks: what a B200's 148 SMs hold; also the height of the
 // workspace's table.
+constexpr int kGradMostBlocks = 2 * 148;
+constexpr size_t kGradTableAt = 256;  // (the status word comes first)
 static constexpr int grad_chunks(int dtype, bool vec) { return vec ? (dtype == NSML_F32 ? 2 : 4) : 1; }
 static int grad_threads(int64_t cols, int dtype, bool vec) {
   const int64_t each = 8 * grad_chunks(dtype, vec);
@@ -299,7 +302,7 @@ static int grad_threads(int64_t cols, int dtype, bool vec) {
 }
 static int grad_blocks(int64_t rows, int64_t cols, int dtype, bool vec) {
   const int threads = grad_threads(cols, dtype, vec), teams = threads < kGradBlock ? kGradBlock / threads : 1;
-  const int64_t most = threads <= kGradBlock ? 2 * 148 : 148, need = (rows + teams - 1) / teams;
+  const int64_t most = threads <= kGradBlock ? kGradMostBlocks : kGradMostBlocks / 2, need = (rows + teams - 1) / teams;
   return (int)(need < most ? need : most);
 }
 
@@ -350,13 +353,7 @@ extern "C" {
 
 size_t nsml_q8_rms_norm_backward_workspace_bytes(int64_t cols) {
   if (cols < 1 || cols > NSML_Q8_MAX_NORM_COLS) return 0;
-  int most = 0;
-  for (const int dtype : {NSML_F32, NSML_BF16})
-    for (const bool vec : {false, true}) {
-      const int blocks = grad_blocks(NSML_Q8_MAX_ROWS, cols, dtype, vec);
-      most = blocks > most ? blocks : most;
-    }
-  return align_up((size_t)most * (size_t)cols * 4, 256);
+  return kGradTableAt + align_up((size_t)kGradMostBlocks * (size_t)cols * 4, 256);  // (the same for every width, so that it never shrinks)
 }
 
 int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64_t lddh, const void* h, int64_t ldh,
@@ -378,12 +375,13 @@ int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64
     if (workspace_bytes < nsml_q8_rms_norm_backward_workspace_bytes(cols)) return NSML_ERR_CAPACITY;
   }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  float* const table = dweight != nullptr ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kGradTableAt) : nullptr;
   const bool vec = cols % 8 == 0 && rows16(dy, ldy, dtype) && rows16(dx, lddx, dtype) && aligned(weight, 16) &&
                    (dh == nullptr || rows16(dh, lddh, dtype)) && (h == nullptr || rows16(h, ldh, dtype));
   if (rows > 0) {
     NormGradArgs a = {};
     a.dy = dy; a.dh = dh; a.h = h; a.codes = codes; a.scales = scales; a.rstd = rstd; a.weight = weight; a.dx = dx;
-    a.partial = dweight != nullptr ? static_cast<float*>(workspace) : nullptr;
+    a.partial = table;
     a.rows = rows; a.cols = (int)cols; a.ldy = ldy; a.lddh = lddh; a.ldh = ldh; a.ldq = ldq; a.lddx = lddx;
     a.weight_bf16 = weight_dtype == NSML_BF16;
     const bool packed = codes != nullptr;
@@ -403,8 +401,8 @@ int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64
   if (dweight != nullptr) {
     LaunchScope scope(K_Q8_NORM_WEIGHT, st);
     const cudaError_t e = launch_prio(k_q8_norm_weight, dim3((unsigned int)((cols + 31) / 32)), dim3(1024), 0, st, false, 0, true, true,
-                                      static_cast<const float*>(workspace), grad_blocks(rows, cols, dtype, vec), cols, dweight,
-                                      dweight_dtype == NSML_BF16, zero_first != 0);
+                                      static_cast<const float*>(table), grad_blocks(rows, cols, dtype, vec), cols, dweight,
+                                      dweight_dtype == NSML_BF16, zero_first != 0, static_cast<int*>(workspace));
     if (e != cudaSuccess) return cuda_error();
   }
   return NSML_OK;

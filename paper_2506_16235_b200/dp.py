@@ -157,6 +157,10 @@ class NormLinear:
     rows, the reciprocal norms and the residual stream in 8 bits: two bytes per element.  The backward pass writes the gradients
     of the norm's weight and of the weight into bucket[offset : offset + size], ready for GradientExchange.step.  CUDA only.
 
+    A backward pass belongs to the last forward pass (what an earlier one kept is gone), with the weights that it used.
+    nsml_last_status of workspaces[0], [1] and [2] tells whether the forward product, the weight's gradient and the input's
+    were completed.
+
     weight [n, k] and norm_weight [k]: float32 or bfloat16 tensors that the optimiser owns; call pack() after it has changed
     them.  bucket: flat float32 or bfloat16 gradient bucket."""
 
@@ -175,8 +179,9 @@ class NormLinear:
         self.grad_norm_weight = bucket[offset:offset + k]
         self.grad_weight = bucket[offset + k:offset + k + n * k].view(n, k)
         self.codes, self.scales = nsml.nsml_q8_empty(n, k, weight.device)
-        self.workspace = nsml.alloc_bytes(max(nsml.NSML_Q8_MATMUL_WORKSPACE_BYTES, int(nsml.lib.nsml_q8_rms_norm_backward_workspace_bytes(k))),
-                                          weight.device)
+        each = nsml.NSML_Q8_MATMUL_WORKSPACE_BYTES
+        workspace = nsml.alloc_bytes(3 * each + int(nsml.lib.nsml_q8_rms_norm_backward_workspace_bytes(k)), weight.device)
+        self.workspaces, self.norm_workspace = tuple(workspace[i * each:(i + 1) * each] for i in range(3)), workspace[3 * each:]
         self.kept = None
         self.pack()
 
@@ -188,7 +193,7 @@ class NormLinear:
         """x, residual [m, k] -> y [m, n] of x's type and h = x + residual (x itself without a residual)."""
         rows, scales, rstd, h = self.nsml.nsml_q8_rms_norm(x, self.norm_weight, self.eps, residual=residual)
         self.kept = rows, scales, rstd, self.nsml.nsml_q8_pack(h)
-        return self.nsml.nsml_q8_matmul(rows, scales, self.codes, self.scales, dtype=x.dtype, workspace=self.workspace), h
+        return self.nsml.nsml_q8_matmul(rows, scales, self.codes, self.scales, dtype=x.dtype, workspace=self.workspaces[0]), h
 
     def backward(self, dy: torch.Tensor, dh: torch.Tensor = None, zero_first: bool = True) -> torch.Tensor:
         """dy [m, n] (bfloat16, n a multiple of 8): writes (zero_first=False: adds) the weights' gradients and returns the
@@ -198,7 +203,7 @@ class NormLinear:
             raise RuntimeError("backward() without a forward() before it")
         (rows, scales, rstd, (h_codes, h_scales)), self.kept = self.kept, None
         nsml = self.nsml
-        nsml.nsml_q8_matmul_grad_weight(dy, rows, scales, dw=self.grad_weight, zero_first=zero_first, workspace=self.workspace)
-        dnormed = nsml.nsml_q8_matmul_grad_input(dy, self.codes, self.scales, workspace=self.workspace)
+        nsml.nsml_q8_matmul_grad_weight(dy, rows, scales, dw=self.grad_weight, zero_first=zero_first, workspace=self.workspaces[1])
+        dnormed = nsml.nsml_q8_matmul_grad_input(dy, self.codes, self.scales, workspace=self.workspaces[2])
         return nsml.nsml_q8_rms_norm_backward(dnormed, self.norm_weight, rstd, codes=h_codes, scales=h_scales, dh=dh, dx=dnormed,
-                                              dweight=self.grad_norm_weight, zero_first=zero_first, workspace=self.workspace)[0]
+                                              dweight=self.grad_norm_weight, zero_first=zero_first, workspace=self.norm_workspace)[0]

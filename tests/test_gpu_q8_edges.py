@@ -204,3 +204,13 @@ def test_narrow_and_empty_products():
         dy = gradient(m, n, 3)
         check(nsml.nsml_q8_matmul_grad_input(dy, b, sb, dtype=torch.float32), f64(dy) @ restored(b, sb), np.abs(f64(dy)) @ np.abs(restored(b, sb)), n, torch.float32)
         check(nsml.nsml_q8_matmul_grad_weight(dy, a, sa), f64(dy).T @ restored(a, sa), np.abs(f64(dy).T) @ np.abs(restored(a, sa)), m, torch.float32)
+
+
+def test_the_norms_gradient_leaves_a_status():
+    cols = 40
+    h, weight = torch.randn(5, cols, generator=torch.Generator().manual_seed(1)).cuda(), torch.ones(cols, device="cuda")
+    rstd = nsml.nsml_q8_rms_norm(h, weight)[2]
+    for rows in (5, 0):
+        ws = nsml.alloc_bytes(int(nsml.lib.nsml_q8_rms_norm_backward_workspace_bytes(cols)), "cuda").fill_(0x55)
+        nsml.nsml_q8_rms_norm_backward(h[:rows], weight, rstd[:rows], h=h[:rows], workspace=ws)
+        assert nsml.nsml_last_status(ws) == 0

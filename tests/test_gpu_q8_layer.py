@@ -97,3 +97,12 @@ def test_refusals():
     block.backward(rand(4, 16, 1))
     with pytest.raises(RuntimeError, match="forward"):  # what was kept is gone
         block.backward(rand(4, 16, 1))
+
+
+def test_status_of_every_product():
+    block, _ = layer(16, 32)
+    for ws in (*block.workspaces, block.norm_workspace):
+        ws.fill_(0x55)
+    block.forward(rand(4, 32, 1))
+    block.backward(rand(4, 16, 1))
+    assert [nsml.nsml_last_status(ws) for ws in (*block.workspaces, block.norm_workspace)] == [0, 0, 0, 0]

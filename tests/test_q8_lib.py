@@ -84,6 +84,11 @@ def test_row_bytes():
     assert [nsml.nsml_q8_row_bytes(c) for c in (0, -1, 1, 16, 17, 2147483632, 2147483633)] == [0, 0, 16, 16, 32, 2147483632, 0]
 
 
+def test_the_norms_workspace_never_shrinks_with_the_width():
+    sizes = [int(lib.nsml_q8_rms_norm_backward_workspace_bytes(c)) for c in range(1, 32769)]
+    assert sizes == sorted(sizes) and sizes[0] >= 256
+
+
 def test_pack_and_unpack_refuse(at):
     good = dict(x=at, rows=4, cols=20, ldx=20, dtype=0, codes=at, ldq=32, scales=at)
 
