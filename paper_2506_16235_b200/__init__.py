@@ -577,6 +577,16 @@ def _workspace(workspace, nbytes: int, device):
     return workspace
 
 
+def _on(stream, call, *args, **kwargs):
+    """The call with `stream` as the current one, so that what it allocates belongs to that stream: memory of another stream
+    could be taken again, or still be in use there, while this one's kernels write it."""
+    torch = _torch()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream.cuda_stream))
+    with torch.cuda.stream(stream):
+        return call(*args, **kwargs)
+
+
 def nsml_q8_row_bytes(cols: int) -> int:
     return int(lib.nsml_q8_row_bytes(int(cols)))
 
@@ -592,6 +602,8 @@ def nsml_q8_empty(rows: int, cols: int, device):
 
 def nsml_q8_pack(x, codes=None, scales=None, stream=None):
     """Stores x (float32 / bfloat16 [rows, cols]) in 8 bits; returns (codes, scales)."""
+    if stream is not None:
+        return _on(stream, nsml_q8_pack, x, codes, scales)
     torch = _torch()
     xp, ldx = _matrix(x, "x")
     rows, cols = x.shape
@@ -600,12 +612,14 @@ def nsml_q8_pack(x, codes=None, scales=None, stream=None):
         codes, scales = new[0] if codes is None else codes, new[1] if scales is None else scales
     cp, ldq = _matrix(codes, "codes", rows, cols, torch.int8)
     sp = _vector(scales, "scales", rows, torch.float32)
-    _check(lib.nsml_q8_pack(xp, rows, cols, ldx, _q8_dtype(x.dtype), cp, ldq, sp, _stream_ptr(stream)), "nsml_q8_pack")
+    _check(lib.nsml_q8_pack(xp, rows, cols, ldx, _q8_dtype(x.dtype), cp, ldq, sp, _stream_ptr(None)), "nsml_q8_pack")
     return codes, scales
 
 
 def nsml_q8_unpack(codes, scales, dtype=None, out=None, stream=None):
     """Restores codes * scales as `dtype` (default: bfloat16), or as out's type into `out`."""
+    if stream is not None:
+        return _on(stream, nsml_q8_unpack, codes, scales, dtype, out)
     torch = _torch()
     cp, ldq = _matrix(codes, "codes", dtype=torch.int8)
     rows, cols = codes.shape
@@ -613,7 +627,7 @@ def nsml_q8_unpack(codes, scales, dtype=None, out=None, stream=None):
     if out is None:
         out = torch.empty(rows, cols, dtype=torch.bfloat16 if dtype is None else dtype, device=codes.device)
     op, ldo = _matrix(out, "out", rows, cols, dtype)
-    _check(lib.nsml_q8_unpack(cp, ldq, sp, rows, cols, op, ldo, _q8_dtype(out.dtype), _stream_ptr(stream)), "nsml_q8_unpack")
+    _check(lib.nsml_q8_unpack(cp, ldq, sp, rows, cols, op, ldo, _q8_dtype(out.dtype), _stream_ptr(None)), "nsml_q8_unpack")
     return out
 
 
@@ -622,6 +636,8 @@ def nsml_q8_rms_norm(x, weight, eps: float = 1e-5, residual=None, h=None, codes=
 
     h is x + residual (a tensor of x's type, allocated unless given; x itself when there is no residual and no h given).
     In place: h may be x or residual."""
+    if stream is not None:
+        return _on(stream, nsml_q8_rms_norm, x, weight, eps, residual, h, codes, scales, rstd)
     torch = _torch()
     xp, ldx = _matrix(x, "x")
     rows, cols = x.shape
@@ -638,7 +654,7 @@ def nsml_q8_rms_norm(x, weight, eps: float = 1e-5, residual=None, h=None, codes=
     if rstd is None:
         rstd = torch.empty(rows, device=x.device)
     _check(lib.nsml_q8_rms_norm(xp, ldx, rp, ldr, rows, cols, _q8_dtype(x.dtype), wp, _q8_dtype(weight.dtype), float(eps), hp, ldh,
-                                cp, ldq, sp, _vector(rstd, "rstd", rows, torch.float32), _stream_ptr(stream)), "nsml_q8_rms_norm")
+                                cp, ldq, sp, _vector(rstd, "rstd", rows, torch.float32), _stream_ptr(None)), "nsml_q8_rms_norm")
     return codes, scales, rstd, x if h is None else h
 
 
@@ -647,6 +663,8 @@ def nsml_q8_rms_norm_backward(dy, weight, rstd, h=None, codes=None, scales=None,
     """Gradient of nsml_q8_rms_norm: returns (dx, dweight).  The normalised rows come as h or as their checkpoint (codes and
     scales of nsml_q8_pack(h)).  dh: a gradient that reaches h past the norm, added to dx.  dweight: float32 / bfloat16
     tensor (a slice of a gradient bucket), float32 and allocated unless given; zero_first=False adds to it."""
+    if stream is not None:
+        return _on(stream, nsml_q8_rms_norm_backward, dy, weight, rstd, h, codes, scales, dh, dx, dweight, zero_first, workspace)
     torch = _torch()
     dyp, ldy = _matrix(dy, "dy")
     rows, cols = dy.shape
@@ -667,12 +685,14 @@ def nsml_q8_rms_norm_backward(dy, weight, rstd, h=None, codes=None, scales=None,
     workspace = _workspace(workspace, int(lib.nsml_q8_rms_norm_backward_workspace_bytes(cols)), dy.device)
     _check(lib.nsml_q8_rms_norm_backward(dyp, ldy, dhp, lddh, hp if rows else None, ldh, cp, ldq, sp, rp, rows, cols, _q8_dtype(dy.dtype), wp,
                                          _q8_dtype(weight.dtype), dxp, lddx, dwp, _q8_dtype(dweight.dtype), 1 if zero_first else 0,
-                                         workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)), "nsml_q8_rms_norm_backward")
+                                         workspace.data_ptr(), workspace.numel(), _stream_ptr(None)), "nsml_q8_rms_norm_backward")
     return dx, dweight
 
 
 def nsml_q8_matmul(a, a_scales, b, b_scales, out=None, dtype=None, workspace=None, stream=None):
     """Activations a [m, k] times weights b [n, k], both q8: out [m, n] (bfloat16 unless dtype or out says float32)."""
+    if stream is not None:
+        return _on(stream, nsml_q8_matmul, a, a_scales, b, b_scales, out, dtype, workspace)
     torch = _torch()
     ap, lda = _matrix(a, "a", dtype=torch.int8)
     m, k = a.shape
@@ -683,12 +703,14 @@ def nsml_q8_matmul(a, a_scales, b, b_scales, out=None, dtype=None, workspace=Non
     op, ldo = _matrix(out, "out", m, n, dtype)
     workspace = _workspace(workspace, NSML_Q8_MATMUL_WORKSPACE_BYTES, a.device)
     _check(lib.nsml_q8_matmul(ap, lda, _vector(a_scales, "a_scales", m, torch.float32), bp, ldb, _vector(b_scales, "b_scales", n, torch.float32),
-                              m, n, k, op, ldo, _q8_dtype(out.dtype), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)), "nsml_q8_matmul")
+                              m, n, k, op, ldo, _q8_dtype(out.dtype), workspace.data_ptr(), workspace.numel(), _stream_ptr(None)), "nsml_q8_matmul")
     return out
 
 
 def nsml_q8_matmul_grad_input(dy, b, b_scales, dx=None, dtype=None, workspace=None, stream=None):
     """dx [m, k] = dy [m, n] (bfloat16, rows a multiple of 16 bytes apart) times the 8-bit weights b [n, k]."""
+    if stream is not None:
+        return _on(stream, nsml_q8_matmul_grad_input, dy, b, b_scales, dx, dtype, workspace)
     torch = _torch()
     dyp, ldy = _matrix(dy, "dy", dtype=torch.bfloat16)
     m, n = dy.shape
@@ -699,7 +721,7 @@ def nsml_q8_matmul_grad_input(dy, b, b_scales, dx=None, dtype=None, workspace=No
     dxp, lddx = _matrix(dx, "dx", m, k, dtype)
     workspace = _workspace(workspace, NSML_Q8_MATMUL_WORKSPACE_BYTES, dy.device)
     _check(lib.nsml_q8_matmul_grad_input(dyp, ldy, bp, ldb, _vector(b_scales, "b_scales", n, torch.float32), m, n, k, dxp, lddx,
-                                         _q8_dtype(dx.dtype), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)),
+                                         _q8_dtype(dx.dtype), workspace.data_ptr(), workspace.numel(), _stream_ptr(None)),
            "nsml_q8_matmul_grad_input")
     return dx
 
@@ -707,6 +729,8 @@ def nsml_q8_matmul_grad_input(dy, b, b_scales, dx=None, dtype=None, workspace=No
 def nsml_q8_matmul_grad_weight(dy, a, a_scales, dw=None, dtype=None, zero_first: bool = True, workspace=None, stream=None):
     """dw [n, k] = dy [m, n] (bfloat16, rows a multiple of 16 bytes apart) transposed times the 8-bit activations a [m, k].
     dw: float32 / bfloat16, any row stride (a slice of a gradient bucket); zero_first=False adds to it."""
+    if stream is not None:
+        return _on(stream, nsml_q8_matmul_grad_weight, dy, a, a_scales, dw, dtype, zero_first, workspace)
     torch = _torch()
     dyp, ldy = _matrix(dy, "dy", dtype=torch.bfloat16)
     m, n = dy.shape
@@ -719,7 +743,7 @@ def nsml_q8_matmul_grad_weight(dy, a, a_scales, dw=None, dtype=None, zero_first:
     workspace = _workspace(workspace, NSML_Q8_MATMUL_WORKSPACE_BYTES, dy.device)
     _check(lib.nsml_q8_matmul_grad_weight(dyp, ldy, ap, lda, _vector(a_scales, "a_scales", m, torch.float32), m, n, k, dwp, lddw,
                                           _q8_dtype(dw.dtype), 1 if zero_first else 0, workspace.data_ptr(), workspace.numel(),
-                                          _stream_ptr(stream)), "nsml_q8_matmul_grad_weight")
+                                          _stream_ptr(None)), "nsml_q8_matmul_grad_weight")
     return dw
 
 

@@ -214,3 +214,19 @@ def test_the_norms_gradient_leaves_a_status():
         ws = nsml.alloc_bytes(int(nsml.lib.nsml_q8_rms_norm_backward_workspace_bytes(cols)), "cuda").fill_(0x55)
         nsml.nsml_q8_rms_norm_backward(h[:rows], weight, rstd[:rows], h=h[:rows], workspace=ws)
         assert nsml.nsml_last_status(ws) == 0
+
+
+def test_what_a_call_allocates_belongs_to_its_stream():
+    # the call waits on its stream; memory that the current stream is given meanwhile is not the call's
+    h = torch.randn(600, 2048, generator=torch.Generator().manual_seed(1)).cuda()
+    weight, stream = torch.ones(2048, device="cuda"), torch.cuda.Stream()
+    rstd = nsml.nsml_q8_rms_norm(h, weight)[2]
+    want, need = nsml.nsml_q8_rms_norm_backward(h, weight, rstd, h=h), int(nsml.lib.nsml_q8_rms_norm_backward_workspace_bytes(2048))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(100_000_000)
+    got = nsml.nsml_q8_rms_norm_backward(h, weight, rstd, h=h, stream=stream)
+    other = [torch.full((need,), 0x55, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert all(bool((o == 0x55).all()) for o in other)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
