@@ -716,13 +716,25 @@ static EncodeTiled encoder() {  // found in the driver, so that the library need
   return f;
 }
 
+// Encodes a map.  The driver wants a context for that, which a host thread that has made no other call does not have yet (a
+// launch would bind the device's): the device is set, then.
+template <class Encode>
+static bool encoded(Encode encode) {
+  CUresult r = encode();
+  int dev = 0;
+  if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess) r = encode();
+  return r == CUDA_SUCCESS;
+}
+
 // `count` scales, from the 16-byte boundary at or before them; boxes of 68.
 static bool scales_map(CUtensorMap* map, const float* scales, int64_t count, int* shift) {
   *shift = (int)(reinterpret_cast<uintptr_t>(scales) % 16 / 4);
   const cuuint64_t dims[1] = {(cuuint64_t)(count + *shift)}, strides[1] = {0};
   const cuuint32_t box[1] = {68}, step[1] = {1};
-  return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 1, const_cast<float*>(scales - *shift), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                   CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return encoded([&] {
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 1, const_cast<float*>(scales - *shift), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  });
 }
 
 // rows x cols elements; boxes of box_cols x box_rows.  What lies outside reads as 0.
@@ -731,9 +743,11 @@ static bool tensor_map(CUtensorMap* map, const void* p, bool codes, int64_t rows
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? ld : (cols * size + 15) / 16 * 16 / size) * size};  // (one row: any stride will do)
   const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, step[2] = {1, 1};
-  return encoder()(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, step,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return encoded([&] {
+    return encoder()(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, step,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  });
 }
 
 struct GemmDevice {

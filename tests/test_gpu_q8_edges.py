@@ -230,3 +230,25 @@ def test_what_a_call_allocates_belongs_to_its_stream():
     torch.cuda.synchronize()
     assert all(bool((o == 0x55).all()) for o in other)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_thread_that_has_made_no_call_before():
+    a, sa = codes_matrix(300, 400, 1)
+    b, sb = codes_matrix(504, 400, 2)
+    dy = gradient(300, 504, 3)
+    want = (nsml.nsml_q8_matmul(a, sa, b, sb), nsml.nsml_q8_matmul_grad_input(dy, b, sb), nsml.nsml_q8_matmul_grad_weight(dy, a, sa))
+    outs, ws, got = [torch.zeros_like(w) for w in want], nsml.alloc_bytes(256, "cuda"), []
+    torch.cuda.synchronize()
+
+    def ptr(t):
+        return t.data_ptr(), t.stride(0)
+
+    calls = (lambda: nsml.lib.nsml_q8_matmul(*ptr(a), sa.data_ptr(), *ptr(b), sb.data_ptr(), 300, 504, 400, *ptr(outs[0]), nsml.NSML_BF16, ws.data_ptr(), 256, 0),
+             lambda: nsml.lib.nsml_q8_matmul_grad_input(*ptr(dy), *ptr(b), sb.data_ptr(), 300, 504, 400, *ptr(outs[1]), nsml.NSML_BF16, ws.data_ptr(), 256, 0),
+             lambda: nsml.lib.nsml_q8_matmul_grad_weight(*ptr(dy), *ptr(a), sa.data_ptr(), 300, 504, 400, *ptr(outs[2]), nsml.NSML_F32, 1, ws.data_ptr(), 256, 0))
+    for call in calls:  # (a thread of its own for each)
+        thread = threading.Thread(target=lambda: got.append(call()))
+        thread.start()
+        thread.join()
+    torch.cuda.synchronize()
+    assert got == [0, 0, 0] and all(torch.equal(o, w) for o, w in zip(outs, want))
