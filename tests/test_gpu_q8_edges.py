@@ -1,6 +1,8 @@
 """Training in 8 bits on the GPU where it goes wrong first: both forms of the products, sums in several pieces, scales off 16-byte
 boundaries, offsets past 32 bits, streams, threads and captured graphs.  Tolerances as in test_gpu_q8.py: u = 2^-24; sums on the
 tensor cores are off by at most a step of every addition, depth * 2u * sum |terms|."""
+import subprocess
+import sys
 import threading
 
 import numpy as np
@@ -252,3 +254,35 @@ def test_a_thread_that_has_made_no_call_before():
         thread.join()
     torch.cuda.synchronize()
     assert got == [0, 0, 0] and all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+FIRST_CALLS_IN_A_CAPTURE = """
+import torch
+import paper_2506_16235_b200 as nsml
+m, n, k = 260, 264, 2048
+x, w, dy = torch.randn(m, k, device="cuda"), torch.randn(n, k, device="cuda"), torch.randn(m, n, device="cuda").bfloat16()
+weight, ws = torch.ones(k, device="cuda"), nsml.alloc_bytes(int(nsml.lib.nsml_q8_rms_norm_backward_workspace_bytes(k)), "cuda")
+def step():
+    codes, scales, rstd, h = nsml.nsml_q8_rms_norm(x, weight)
+    b, sb = nsml.nsml_q8_pack(w)
+    y = nsml.nsml_q8_matmul(codes, scales, b, sb)
+    token = nsml.nsml_q8_matmul(codes[:1], scales[:1], b, sb)
+    dw = nsml.nsml_q8_matmul_grad_weight(dy, codes, scales)
+    dx = nsml.nsml_q8_matmul_grad_input(dy, b, sb, dtype=torch.float32)
+    return y, token, dw, *nsml.nsml_q8_rms_norm_backward(dx, weight, rstd, h=h, workspace=ws), nsml.nsml_q8_unpack(codes, scales)
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    got = step()
+for _ in range(2):
+    graph.replay()
+want = step()
+torch.cuda.synchronize()
+assert all(torch.equal(g, w) for g, w in zip(got, want))
+print("equal")
+"""
+
+
+def test_a_programs_first_calls_are_captured():
+    done = subprocess.run([sys.executable, "-c", FIRST_CALLS_IN_A_CAPTURE], capture_output=True, text=True, timeout=120)
+    assert done.returncode == 0 and done.stdout.strip() == "equal", done.stderr[-2000:]
