@@ -152,6 +152,7 @@ def _load() -> ctypes.CDLL:
 
 
 lib = _load()
+from . import _native  # noqa: E402  (linked to the library; built with it)
 
 
 def nsml_strerror(status: int) -> str:
@@ -270,6 +271,7 @@ def _torch():
             _raw_stream = lambda: int(torch.cuda.current_stream().cuda_stream)  # noqa: E731
         # (without a device every tensor is refused by its own index, -1)
         _device_index = (device or torch.cuda.current_device) if torch.cuda.is_available() else lambda: 0
+        _native.setup(torch.float32, torch.bfloat16, torch.int8, _device_index, get or (lambda index: _raw_stream()))
         _torch_module = torch
     return _torch_module
 
@@ -529,52 +531,16 @@ def nsml_decompress_accumulate_host(payloads_host: Sequence, dense_host, zero_fi
 NSML_Q8_MATMUL_WORKSPACE_BYTES = 256
 
 
-def _matrix(t, what: str, rows: Optional[int] = None, cols: Optional[int] = None, dtype=None):
-    """Checks a 2-D CUDA tensor of the current device with contiguous rows; returns (pointer, row stride)."""
+def _rows(t, what: str):
+    """The shape of a 2-D tensor that a call is to allocate its results for; the call checks the rest."""
     if t.dim() != 2:
         raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
-    (r, c), (ld, inner) = t.shape, t.stride()
-    if inner != 1 and c > 1:
-        raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
-    if (rows is not None and r != rows) or (cols is not None and c != cols):
-        raise ValueError(f"{what} must have shape ({rows}, {cols}), not ({r}, {c})")
+    return t.shape
+
+
+def _same_type(t, what: str, dtype) -> None:
     if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
-    if t.get_device() != (_device_index or _device_query())():
-        raise ValueError(f"{what} must be a tensor of the current CUDA device")
-    return t.data_ptr(), ld
-
-
-def _vector(t, what: str, n: int, dtype=None):
-    if t.dim() != 1 or t.numel() != n or (n > 1 and not t.is_contiguous()):
-        raise ValueError(f"{what} must be a contiguous 1-D tensor of {n} elements")
-    if dtype is not None and t.dtype is not dtype:
-        raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
-    if t.get_device() != (_device_index or _device_query())():
-        raise ValueError(f"{what} must be a tensor of the current CUDA device")
-    return t.data_ptr()
-
-
-def _device_query():
-    _torch()
-    return _device_index
-
-
-def _q8_dtype(dtype) -> int:
-    torch = _torch_module or _torch()
-    if dtype is torch.bfloat16:
-        return NSML_BF16
-    if dtype is torch.float32:
-        return NSML_F32
-    raise TypeError("matrices must be float32 or bfloat16")
-
-
-def _workspace(workspace, nbytes: int, device):
-    if workspace is None:
-        return alloc_bytes(nbytes, device)
-    if workspace.get_device() != _device_query()():
-        raise ValueError("workspace must be a tensor of the current CUDA device")
-    return workspace
 
 
 def _on(stream, call, *args, **kwargs):
@@ -604,15 +570,11 @@ def nsml_q8_pack(x, codes=None, scales=None, stream=None):
     """Stores x (float32 / bfloat16 [rows, cols]) in 8 bits; returns (codes, scales)."""
     if stream is not None:
         return _on(stream, nsml_q8_pack, x, codes, scales)
-    torch = _torch()
-    xp, ldx = _matrix(x, "x")
-    rows, cols = x.shape
     if codes is None or scales is None:
-        new = nsml_q8_empty(rows, cols, x.device)
+        new = nsml_q8_empty(*_rows(x, "x"), x.device)
         codes, scales = new[0] if codes is None else codes, new[1] if scales is None else scales
-    cp, ldq = _matrix(codes, "codes", rows, cols, torch.int8)
-    sp = _vector(scales, "scales", rows, torch.float32)
-    _check(lib.nsml_q8_pack(xp, rows, cols, ldx, _q8_dtype(x.dtype), cp, ldq, sp, _stream_ptr(None)), "nsml_q8_pack")
+    _torch_module or _torch()
+    _check(_native.pack(x, codes, scales), "nsml_q8_pack")
     return codes, scales
 
 
@@ -620,14 +582,12 @@ def nsml_q8_unpack(codes, scales, dtype=None, out=None, stream=None):
     """Restores codes * scales as `dtype` (default: bfloat16), or as out's type into `out`."""
     if stream is not None:
         return _on(stream, nsml_q8_unpack, codes, scales, dtype, out)
-    torch = _torch()
-    cp, ldq = _matrix(codes, "codes", dtype=torch.int8)
-    rows, cols = codes.shape
-    sp = _vector(scales, "scales", rows, torch.float32)
+    torch = _torch_module or _torch()
     if out is None:
-        out = torch.empty(rows, cols, dtype=torch.bfloat16 if dtype is None else dtype, device=codes.device)
-    op, ldo = _matrix(out, "out", rows, cols, dtype)
-    _check(lib.nsml_q8_unpack(cp, ldq, sp, rows, cols, op, ldo, _q8_dtype(out.dtype), _stream_ptr(None)), "nsml_q8_unpack")
+        out = torch.empty(_rows(codes, "codes"), dtype=torch.bfloat16 if dtype is None else dtype, device=codes.device)
+    else:
+        _same_type(out, "out", dtype)
+    _check(_native.unpack(codes, scales, out), "nsml_q8_unpack")
     return out
 
 
@@ -638,23 +598,15 @@ def nsml_q8_rms_norm(x, weight, eps: float = 1e-5, residual=None, h=None, codes=
     In place: h may be x or residual."""
     if stream is not None:
         return _on(stream, nsml_q8_rms_norm, x, weight, eps, residual, h, codes, scales, rstd)
-    torch = _torch()
-    xp, ldx = _matrix(x, "x")
-    rows, cols = x.shape
-    wp = _vector(weight, "weight", cols)
-    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", rows, cols, x.dtype)
+    torch = _torch_module or _torch()
     if h is None and residual is not None:
-        h = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
-    hp, ldh = (None, 0) if h is None else _matrix(h, "h", rows, cols, x.dtype)
+        h = torch.empty(_rows(x, "x"), dtype=x.dtype, device=x.device)
     if codes is None or scales is None:
-        new = nsml_q8_empty(rows, cols, x.device)
+        new = nsml_q8_empty(*_rows(x, "x"), x.device)
         codes, scales = new[0] if codes is None else codes, new[1] if scales is None else scales
-    cp, ldq = _matrix(codes, "codes", rows, cols, torch.int8)
-    sp = _vector(scales, "scales", rows, torch.float32)
     if rstd is None:
-        rstd = torch.empty(rows, device=x.device)
-    _check(lib.nsml_q8_rms_norm(xp, ldx, rp, ldr, rows, cols, _q8_dtype(x.dtype), wp, _q8_dtype(weight.dtype), float(eps), hp, ldh,
-                                cp, ldq, sp, _vector(rstd, "rstd", rows, torch.float32), _stream_ptr(None)), "nsml_q8_rms_norm")
+        rstd = torch.empty(_rows(x, "x")[0], device=x.device)
+    _check(_native.rms_norm(x, weight, eps, residual, h, codes, scales, rstd), "nsml_q8_rms_norm")
     return codes, scales, rstd, x if h is None else h
 
 
@@ -665,27 +617,15 @@ def nsml_q8_rms_norm_backward(dy, weight, rstd, h=None, codes=None, scales=None,
     tensor (a slice of a gradient bucket), float32 and allocated unless given; zero_first=False adds to it."""
     if stream is not None:
         return _on(stream, nsml_q8_rms_norm_backward, dy, weight, rstd, h, codes, scales, dh, dx, dweight, zero_first, workspace)
-    torch = _torch()
-    dyp, ldy = _matrix(dy, "dy")
-    rows, cols = dy.shape
-    if (h is None) == (codes is None):
-        raise ValueError("give h, or codes and scales")
-    wp, rp = _vector(weight, "weight", cols), _vector(rstd, "rstd", rows, torch.float32)
-    hp, ldh = (None, 0) if h is None else _matrix(h, "h", rows, cols, dy.dtype)
-    cp, ldq = (None, 0) if codes is None else _matrix(codes, "codes", rows, cols, torch.int8)
-    sp = None if codes is None else _vector(scales, "scales", rows, torch.float32)
-    dhp, lddh = (None, 0) if dh is None else _matrix(dh, "dh", rows, cols, dy.dtype)
+    torch = _torch_module or _torch()
     if dx is None:
-        dx = torch.empty(rows, cols, dtype=dy.dtype, device=dy.device)
-    dxp, lddx = _matrix(dx, "dx", rows, cols, dy.dtype)
+        dx = torch.empty(_rows(dy, "dy"), dtype=dy.dtype, device=dy.device)
     if dweight is None:
-        dweight = torch.empty(cols, device=dy.device)
+        dweight = torch.empty(_rows(dy, "dy")[1], device=dy.device)
         zero_first = True
-    dwp = _vector(dweight, "dweight", cols)
-    workspace = _workspace(workspace, int(lib.nsml_q8_rms_norm_backward_workspace_bytes(cols)), dy.device)
-    _check(lib.nsml_q8_rms_norm_backward(dyp, ldy, dhp, lddh, hp if rows else None, ldh, cp, ldq, sp, rp, rows, cols, _q8_dtype(dy.dtype), wp,
-                                         _q8_dtype(weight.dtype), dxp, lddx, dwp, _q8_dtype(dweight.dtype), 1 if zero_first else 0,
-                                         workspace.data_ptr(), workspace.numel(), _stream_ptr(None)), "nsml_q8_rms_norm_backward")
+    if workspace is None:
+        workspace = alloc_bytes(int(lib.nsml_q8_rms_norm_backward_workspace_bytes(_rows(dy, "dy")[1])), dy.device)
+    _check(_native.rms_norm_backward(dy, weight, rstd, h, codes, scales, dh, dx, dweight, zero_first, workspace), "nsml_q8_rms_norm_backward")
     return dx, dweight
 
 
@@ -693,17 +633,14 @@ def nsml_q8_matmul(a, a_scales, b, b_scales, out=None, dtype=None, workspace=Non
     """Activations a [m, k] times weights b [n, k], both q8: out [m, n] (bfloat16 unless dtype or out says float32)."""
     if stream is not None:
         return _on(stream, nsml_q8_matmul, a, a_scales, b, b_scales, out, dtype, workspace)
-    torch = _torch()
-    ap, lda = _matrix(a, "a", dtype=torch.int8)
-    m, k = a.shape
-    bp, ldb = _matrix(b, "b", b.shape[0], k, torch.int8)
-    n = b.shape[0]
+    torch = _torch_module or _torch()
     if out is None:
-        out = torch.empty(m, n, dtype=torch.bfloat16 if dtype is None else dtype, device=a.device)
-    op, ldo = _matrix(out, "out", m, n, dtype)
-    workspace = _workspace(workspace, NSML_Q8_MATMUL_WORKSPACE_BYTES, a.device)
-    _check(lib.nsml_q8_matmul(ap, lda, _vector(a_scales, "a_scales", m, torch.float32), bp, ldb, _vector(b_scales, "b_scales", n, torch.float32),
-                              m, n, k, op, ldo, _q8_dtype(out.dtype), workspace.data_ptr(), workspace.numel(), _stream_ptr(None)), "nsml_q8_matmul")
+        out = torch.empty(_rows(a, "a")[0], _rows(b, "b")[0], dtype=torch.bfloat16 if dtype is None else dtype, device=a.device)
+    else:
+        _same_type(out, "out", dtype)
+    if workspace is None:
+        workspace = alloc_bytes(NSML_Q8_MATMUL_WORKSPACE_BYTES, a.device)
+    _check(_native.matmul(a, a_scales, b, b_scales, out, workspace), "nsml_q8_matmul")
     return out
 
 
@@ -711,18 +648,14 @@ def nsml_q8_matmul_grad_input(dy, b, b_scales, dx=None, dtype=None, workspace=No
     """dx [m, k] = dy [m, n] (bfloat16, rows a multiple of 16 bytes apart) times the 8-bit weights b [n, k]."""
     if stream is not None:
         return _on(stream, nsml_q8_matmul_grad_input, dy, b, b_scales, dx, dtype, workspace)
-    torch = _torch()
-    dyp, ldy = _matrix(dy, "dy", dtype=torch.bfloat16)
-    m, n = dy.shape
-    bp, ldb = _matrix(b, "b", n, b.shape[-1], torch.int8)
-    k = b.shape[1]
+    torch = _torch_module or _torch()
     if dx is None:
-        dx = torch.empty(m, k, dtype=torch.bfloat16 if dtype is None else dtype, device=dy.device)
-    dxp, lddx = _matrix(dx, "dx", m, k, dtype)
-    workspace = _workspace(workspace, NSML_Q8_MATMUL_WORKSPACE_BYTES, dy.device)
-    _check(lib.nsml_q8_matmul_grad_input(dyp, ldy, bp, ldb, _vector(b_scales, "b_scales", n, torch.float32), m, n, k, dxp, lddx,
-                                         _q8_dtype(dx.dtype), workspace.data_ptr(), workspace.numel(), _stream_ptr(None)),
-           "nsml_q8_matmul_grad_input")
+        dx = torch.empty(_rows(dy, "dy")[0], _rows(b, "b")[1], dtype=torch.bfloat16 if dtype is None else dtype, device=dy.device)
+    else:
+        _same_type(dx, "dx", dtype)
+    if workspace is None:
+        workspace = alloc_bytes(NSML_Q8_MATMUL_WORKSPACE_BYTES, dy.device)
+    _check(_native.grad_input(dy, b, b_scales, dx, workspace), "nsml_q8_matmul_grad_input")
     return dx
 
 
@@ -731,19 +664,15 @@ def nsml_q8_matmul_grad_weight(dy, a, a_scales, dw=None, dtype=None, zero_first:
     dw: float32 / bfloat16, any row stride (a slice of a gradient bucket); zero_first=False adds to it."""
     if stream is not None:
         return _on(stream, nsml_q8_matmul_grad_weight, dy, a, a_scales, dw, dtype, zero_first, workspace)
-    torch = _torch()
-    dyp, ldy = _matrix(dy, "dy", dtype=torch.bfloat16)
-    m, n = dy.shape
-    ap, lda = _matrix(a, "a", m, a.shape[-1], torch.int8)
-    k = a.shape[1]
+    torch = _torch_module or _torch()
     if dw is None:
-        dw = torch.empty(n, k, dtype=torch.float32 if dtype is None else dtype, device=dy.device)
+        dw = torch.empty(_rows(dy, "dy")[1], _rows(a, "a")[1], dtype=torch.float32 if dtype is None else dtype, device=dy.device)
         zero_first = True
-    dwp, lddw = _matrix(dw, "dw", n, k, dtype)
-    workspace = _workspace(workspace, NSML_Q8_MATMUL_WORKSPACE_BYTES, dy.device)
-    _check(lib.nsml_q8_matmul_grad_weight(dyp, ldy, ap, lda, _vector(a_scales, "a_scales", m, torch.float32), m, n, k, dwp, lddw,
-                                          _q8_dtype(dw.dtype), 1 if zero_first else 0, workspace.data_ptr(), workspace.numel(),
-                                          _stream_ptr(None)), "nsml_q8_matmul_grad_weight")
+    else:
+        _same_type(dw, "dw", dtype)
+    if workspace is None:
+        workspace = alloc_bytes(NSML_Q8_MATMUL_WORKSPACE_BYTES, dy.device)
+    _check(_native.grad_weight(dy, a, a_scales, dw, zero_first, workspace), "nsml_q8_matmul_grad_weight")
     return dw
 
 

@@ -1,4 +1,5 @@
-"""Builds libnsml.so in-tree with nvcc for sm_100a (cross-compiles without a GPU).
+"""Builds libnsml.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and the module that calls its 8-bit operators
+from Python (the rest goes through ctypes).
 
     python -m paper_2506_16235_b200.build [--force] [--verbose]
 """
@@ -9,6 +10,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
@@ -16,6 +18,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG_DIR, "libnsml.so")
 STAMP_PATH = LIB_PATH + ".stamp"
+NATIVE_PATH = os.path.join(PKG_DIR, "_native" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 SOURCES = ["nsml_api.cu", "nsml_grid_large.cu", "nsml_q8_rows.cu", "nsml_q8_norm_grad.cu", "nsml_q8_gemm.cu", "nsml_q8_tokens.cu", "nsml_controller.cpp"]
 FLAGS = [
@@ -25,6 +28,8 @@ FLAGS = [
     "-Xcompiler", "-fPIC", "-Xcompiler", "-ffp-contract=off",
     "-shared", "-cudart", "static", "--threads", "7",
 ]
+NATIVE_SOURCE = "nsml_python.cpp"
+NATIVE_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-shared", "-Wall"]
 
 
 def _nvcc() -> str:
@@ -48,17 +53,40 @@ def _fingerprint() -> str:
         h.update(os.path.basename(f).encode())
         with open(f, "rb") as fh:
             h.update(fh.read())
-    h.update(" ".join(FLAGS).encode())
+    h.update(" ".join(FLAGS + NATIVE_FLAGS).encode())
     return h.hexdigest()
 
 
 def is_stale() -> bool:
     """True if the library is missing or was built from other sources or flags
     (content hash, so file times do not matter)."""
-    if not (os.path.exists(LIB_PATH) and os.path.exists(STAMP_PATH)):
+    if not all(map(os.path.exists, (LIB_PATH, NATIVE_PATH, STAMP_PATH))):
         return True
     with open(STAMP_PATH) as fh:
         return fh.read().strip() != _fingerprint()
+
+
+def _cxx() -> str:
+    for cand in (os.environ.get("CXX"), shutil.which("g++"), shutil.which("c++")):
+        if cand and shutil.which(cand):
+            return cand
+    raise RuntimeError("no C++ compiler found (set CXX or put g++ on PATH)")
+
+
+def _run(cmd, what: str, verbose: bool) -> None:
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if verbose or res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+    if res.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed building {what}")
+
+
+def build_native(verbose: bool = False) -> None:
+    """The Python module, linked to the library next to it."""
+    tmp = NATIVE_PATH + ".tmp"
+    _run([_cxx()] + NATIVE_FLAGS + ["-I", INCLUDE, "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, NATIVE_SOURCE), "-o", tmp,
+                                    "-L", PKG_DIR, "-l:" + os.path.basename(LIB_PATH), "-Wl,-rpath,$ORIGIN"], os.path.basename(NATIVE_PATH), verbose)
+    os.replace(tmp, NATIVE_PATH)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -71,12 +99,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
     cmd += [os.path.join(CSRC, s) for s in SOURCES]
     tmp = LIB_PATH + ".tmp"
     cmd += ["-o", tmp]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed building libnsml.so")
+    _run(cmd, "libnsml.so", verbose)
     os.replace(tmp, LIB_PATH)
+    build_native(verbose)
     with open(STAMP_PATH, "w") as fh:
         fh.write(_fingerprint() + "\n")
     return LIB_PATH
