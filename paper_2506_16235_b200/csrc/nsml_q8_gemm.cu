@@ -320,18 +320,56 @@ __device__ __forceinline__ void put4(const GemmArgs& g, int64_t row, int64_t col
   }
 }
 
-// The words of 32 rows of 128 bytes that are staged in 16-byte pieces, swizzled: word `lane` of every row below `last`, and where
-// it goes.
+// Word `lane` of a row of 128 bytes that is staged in 16-byte pieces, swizzled.
+__device__ __forceinline__ uint32_t staged(const unsigned char* stage, int rr, int lane) {
+  return *reinterpret_cast<const uint32_t*>(stage + rr * 128 + (((lane >> 2) ^ (rr & 7)) << 4) + 4 * (lane & 3));
+}
+// Those of every row below `last`, and where they go.
 template <class Put>
 __device__ __forceinline__ void each_row(const unsigned char* stage, int lane, int last, unsigned char* to, int64_t pitch, Put put) {
 #pragma unroll 8
   for (int rr = 0; rr < 32; ++rr, to += pitch) {
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(stage + rr * 128 + (((lane >> 2) ^ (rr & 7)) << 4) + 4 * (lane & 3));
+    const uint32_t w = staged(stage, rr, lane);
     if (rr < last) put(to, w);
   }
 }
 
-template <int MODE, bool PAIR>
+// The block of 32 x 32 float32 results on top of what is there, rows below `rows` and columns below `cols`; wide: all of them,
+// and float32 rows on 16-byte boundaries.  What is there is fetched for all rows before the first one is stored (a load may not
+// move past a store: row by row 1024 x 8192 x 2048 took 98 us instead of 51, in bfloat16 171 instead of 64, and 7487 x 385 x 10163,
+// whose rows are off 16-byte boundaries, 275 instead of 127).  A function of its own, so that the rest has the registers.
+template <class T>
+__device__ __forceinline__ void add_rows(const unsigned char* stage, int lane, int last, unsigned char* to, int64_t pitch) {
+  T old[32];
+#pragma unroll
+  for (int rr = 0; rr < 32; ++rr) old[rr] = rr < last ? *reinterpret_cast<const T*>(to + rr * pitch) : T(0.0f);
+#pragma unroll
+  for (int rr = 0; rr < 32; ++rr) {
+    const float v = __fadd_rn(__uint_as_float(staged(stage, rr, lane)), (float)old[rr]);
+    if (rr >= last) continue;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<T*>(to + rr * pitch) = __float2bfloat16_rn(v);
+    else *reinterpret_cast<T*>(to + rr * pitch) = v;
+  }
+}
+__device__ __noinline__ void add_out(const unsigned char* stage, int rows, int cols, unsigned char* to, int64_t pitch, bool bf16, bool wide) {
+  const int lane = threadIdx.x & 31, last = lane < cols ? rows : 0;
+  if (bf16) return add_rows<__nv_bfloat16>(stage, lane, last, to + 2 * lane, pitch);
+  if (!wide) return add_rows<float>(stage, lane, last, to + 4 * lane, pitch);
+  const int j = lane & 7;
+  to += (lane >> 3) * pitch + 16 * j;
+  float4 old[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) old[i] = *reinterpret_cast<const float4*>(to + 4 * i * pitch);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int rr = 4 * i + (lane >> 3);
+    const float4 w = *reinterpret_cast<const float4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
+    *reinterpret_cast<float4*>(to + 4 * i * pitch) = make_float4(__fadd_rn(w.x, old[i].x), __fadd_rn(w.y, old[i].y), __fadd_rn(w.z, old[i].z), __fadd_rn(w.w, old[i].w));
+  }
+}
+
+// ADD (PAIR only): results may go on top of what is there, a piece of the sum on top of the one before it among them.
+template <int MODE, bool PAIR, bool ADD>
 __global__ void __launch_bounds__(Shape<MODE, PAIR>::kThreads, 1)
 k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_scales,
           const GemmArgs g) {
@@ -503,7 +541,7 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
           unsigned char* const stage = out + (warp - 4) * 4096;  // 32 rows of 128 bytes, pieces of 16 swizzled
           float* const scales = reinterpret_cast<float*>(out + S::kOutWarps * 4096) + (warp - 4) * 128;
           const int64_t row0 = m * 256 + rank * 128 + quarter * 32, col0 = n * 256 + first_chunk * 32;
-          const bool add = g.add || piece > from, packed = g.bf16 && !add;
+          const bool add = ADD && (g.add || piece > from), packed = g.bf16 && !add;
           float rs = 0.0f;
           if constexpr (MODE == kForward) {
             rs = row0 + lane < g.rows ? g.row_scale[row0 + lane] : 0.0f;
@@ -549,20 +587,15 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             const int64_t block = col0 + (packed ? c >> 1 : c) * width;
             unsigned char* const corner = static_cast<unsigned char*>(g.out) + (row0 * g.ldo + block) * size;
             const int64_t pitch = g.ldo * size;
-            if (g.vec && row0 + 32 <= g.rows && block + width <= g.cols && (packed || !g.bf16)) {  // 16 bytes per lane, four rows at a time
+            const bool whole = g.vec && row0 + 32 <= g.rows && block + width <= g.cols;
+            if (whole && !add) {  // 16 bytes per lane, four rows at a time
               unsigned char* to = corner + (lane >> 3) * pitch + 16 * (lane & 7);
 #pragma unroll
               for (int i = 0; i < 8; ++i, to += 4 * pitch) {
                 const int rr = 4 * i + (lane >> 3), j = lane & 7;
-                uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
-                if (add) {
-                  const float4 o = *reinterpret_cast<const float4*>(to);
-                  w = make_uint4(__float_as_uint(__fadd_rn(__uint_as_float(w.x), o.x)), __float_as_uint(__fadd_rn(__uint_as_float(w.y), o.y)),
-                                 __float_as_uint(__fadd_rn(__uint_as_float(w.z), o.z)), __float_as_uint(__fadd_rn(__uint_as_float(w.w), o.w)));
-                }
-                *reinterpret_cast<uint4*>(to) = w;
+                *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
               }
-            } else if (packed || (!g.bf16 && !add)) {  // 4 bytes per lane, a row at a time: stores next to each other wherever the row starts
+            } else if (!add) {  // 4 bytes per lane, a row at a time: stores next to each other wherever the row starts
               const int64_t col = block + (packed ? 2 : 1) * lane;
               const int last = col < g.cols ? (int)min((int64_t)32, g.rows - row0) : 0;
               unsigned char* const to = corner + 4 * lane;
@@ -575,16 +608,8 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
                   if (two) reinterpret_cast<uint16_t*>(at)[1] = (uint16_t)(w >> 16);
                 });
               }
-            } else {  // on top of what is there, at the edges, off 16-byte boundaries or in bfloat16
-              each_row(stage, lane, block + lane < g.cols ? (int)min((int64_t)32, g.rows - row0) : 0, corner + size * lane, pitch, [&](unsigned char* at, uint32_t w) {
-                if (g.bf16) {
-                  __nv_bfloat16* const to = reinterpret_cast<__nv_bfloat16*>(at);
-                  *to = __float2bfloat16_rn(add ? __fadd_rn(__uint_as_float(w), (float)*to) : __uint_as_float(w));
-                } else {
-                  float* const to = reinterpret_cast<float*>(at);
-                  *to = __fadd_rn(__uint_as_float(w), *to);
-                }
-              });
+            } else if constexpr (ADD) {  // on top of what is there
+              add_out(stage, (int)min((int64_t)32, g.rows - row0), (int)min((int64_t)32, g.cols - block), corner, pitch, g.bf16, whole);
             }
             __syncwarp();
           }
@@ -758,9 +783,9 @@ static GemmDevice g_gemm_dev[64];
 static std::mutex g_gemm_mutex;
 
 // clusters[s]: how many clusters of 2^s blocks are resident at once (at most what all three modes have)
-template <int MODE, bool PAIR>
+template <int MODE, bool PAIR, bool ADD = false>
 static cudaError_t prepare_kernel(int* clusters) {
-  cudaError_t e = cudaFuncSetAttribute(k_q8_gemm<MODE, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<MODE, PAIR>::kSmem);
+  cudaError_t e = cudaFuncSetAttribute(k_q8_gemm<MODE, PAIR, ADD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<MODE, PAIR>::kSmem);
   for (int s = 0; s <= 3 && e == cudaSuccess; ++s) {
     if (PAIR && s != 1) continue;
     cudaLaunchConfig_t cfg = {};
@@ -774,7 +799,7 @@ static cudaError_t prepare_kernel(int* clusters) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int c = 0;
-    e = cudaOccupancyMaxActiveClusters(&c, k_q8_gemm<MODE, PAIR>, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&c, k_q8_gemm<MODE, PAIR, ADD>, &cfg);
     if (e == cudaSuccess && c < 1) e = cudaErrorUnknown;
     if (clusters[s] == 0 || c < clusters[s]) clusters[s] = c;
   }
@@ -790,6 +815,8 @@ static int gemm_device(const GemmDevice** out) {
     cudaError_t e = prepare_kernel<kForward, true>(d.pairs);
     if (e == cudaSuccess) e = prepare_kernel<kGradInput, true>(d.pairs);
     if (e == cudaSuccess) e = prepare_kernel<kGradWeight, true>(d.pairs);
+    if (e == cudaSuccess) e = prepare_kernel<kGradInput, true, true>(d.pairs);
+    if (e == cudaSuccess) e = prepare_kernel<kGradWeight, true, true>(d.pairs);
     if (e == cudaSuccess) e = prepare_kernel<kForward, false>(d.split);
     if (e == cudaSuccess) e = prepare_kernel<kGradInput, false>(d.split);
     if (e == cudaSuccess) e = prepare_kernel<kGradWeight, false>(d.split);
@@ -833,11 +860,14 @@ static int launch_gemm(const CUtensorMap& map_a, const CUtensorMap& map_b, const
   cudaError_t e;
   if (form == 0) {
     using S = Shape<MODE, true>;
-    e = launch_prio(k_q8_gemm<MODE, true>, dim3((unsigned int)(2 * (tiles < dev.pairs[1] ? tiles : dev.pairs[1]))), dim3(S::kThreads), S::kSmem, st, false, 2,
-                    false, true, map_a, map_b, map_scales, g);
+    auto* kernel = k_q8_gemm<MODE, true, false>;
+    if constexpr (MODE != kForward)
+      if (g.add || g.piece < g.steps) kernel = k_q8_gemm<MODE, true, true>;
+    e = launch_prio(kernel, dim3((unsigned int)(2 * (tiles < dev.pairs[1] ? tiles : dev.pairs[1]))), dim3(S::kThreads), S::kSmem, st, false, 2, false, true, map_a, map_b,
+                    map_scales, g);
   } else {
     using S = Shape<MODE, false>;
-    e = launch_prio(k_q8_gemm<MODE, false>, dim3((unsigned int)(tiles * form)), dim3(S::kThreads), S::kSmem, st, false, (unsigned int)form, false, true,
+    e = launch_prio(k_q8_gemm<MODE, false, false>, dim3((unsigned int)(tiles * form)), dim3(S::kThreads), S::kSmem, st, false, (unsigned int)form, false, true,
                     map_a, map_b, map_scales, g);
   }
   return e == cudaSuccess ? NSML_OK : cuda_error();
