@@ -320,6 +320,14 @@ __device__ __forceinline__ void put4(const GemmArgs& g, int64_t row, int64_t col
   }
 }
 
+// Results that nothing is added to leave L2 first, so that their lines are written as they fill up (8192 x 8192 x 128 in float32
+// 69 us without, 56 with it; beside it, 32 rows in a row without a branch back: 13779 x 9100 x 100 in bfloat16 107 -> 94).
+template <bool KEEP, class T>
+__device__ __forceinline__ void store_out(T* to, T v) {
+  if constexpr (KEEP) *to = v;
+  else __stcs(to, v);
+}
+
 // Word `lane` of a row of 128 bytes that is staged in 16-byte pieces, swizzled.
 __device__ __forceinline__ uint32_t staged(const unsigned char* stage, int rr, int lane) {
   return *reinterpret_cast<const uint32_t*>(stage + rr * 128 + (((lane >> 2) ^ (rr & 7)) << 4) + 4 * (lane & 3));
@@ -327,7 +335,7 @@ __device__ __forceinline__ uint32_t staged(const unsigned char* stage, int rr, i
 // Those of every row below `last`, and where they go.
 template <class Put>
 __device__ __forceinline__ void each_row(const unsigned char* stage, int lane, int last, unsigned char* to, int64_t pitch, Put put) {
-#pragma unroll 8
+#pragma unroll
   for (int rr = 0; rr < 32; ++rr, to += pitch) {
     const uint32_t w = staged(stage, rr, lane);
     if (rr < last) put(to, w);
@@ -593,19 +601,19 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
 #pragma unroll
               for (int i = 0; i < 8; ++i, to += 4 * pitch) {
                 const int rr = 4 * i + (lane >> 3), j = lane & 7;
-                *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4));
+                store_out<ADD>(reinterpret_cast<uint4*>(to), *reinterpret_cast<const uint4*>(stage + rr * 128 + ((j ^ (rr & 7)) << 4)));
               }
             } else if (!add) {  // 4 bytes per lane, a row at a time: stores next to each other wherever the row starts
               const int64_t col = block + (packed ? 2 : 1) * lane;
               const int last = col < g.cols ? (int)min((int64_t)32, g.rows - row0) : 0;
               unsigned char* const to = corner + 4 * lane;
               if (!packed || (g.even && col + 2 <= g.cols)) {
-                each_row(stage, lane, last, to, pitch, [](unsigned char* at, uint32_t w) { *reinterpret_cast<uint32_t*>(at) = w; });
+                each_row(stage, lane, last, to, pitch, [](unsigned char* at, uint32_t w) { store_out<ADD>(reinterpret_cast<uint32_t*>(at), w); });
               } else {
                 const bool two = col + 1 < g.cols;
                 each_row(stage, lane, last, to, pitch, [&](unsigned char* at, uint32_t w) {
-                  reinterpret_cast<uint16_t*>(at)[0] = (uint16_t)w;
-                  if (two) reinterpret_cast<uint16_t*>(at)[1] = (uint16_t)(w >> 16);
+                  store_out<ADD>(reinterpret_cast<uint16_t*>(at), (uint16_t)w);
+                  if (two) store_out<ADD>(reinterpret_cast<uint16_t*>(at) + 1, (uint16_t)(w >> 16));
                 });
               }
             } else if constexpr (ADD) {  // on top of what is there
