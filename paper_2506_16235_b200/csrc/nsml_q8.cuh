@@ -144,8 +144,15 @@ struct Raw8 {
     if constexpr (VEC) {
       if (column<VEC, THREADS>(lane, i, 0) >= (unsigned int)cols) return;
       uint4* to = reinterpret_cast<uint4*>(row + column<VEC, THREADS>(lane, i, 0));
-      to[0] = make_uint4(w[0], w[1], w[2], w[3]);
-      if constexpr (!kPairs) to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      if constexpr (kPairs) {
+        to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      } else if (reinterpret_cast<uintptr_t>(to) % 32 == 0) {  // in one store: two of 16 bytes, 32 apart across the lanes, write half sectors
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+                     "r"(w[6]), "r"(w[7]) : "memory");
+      } else {
+        to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      }
     } else {
       Bits* to = reinterpret_cast<Bits*>(row) + lane;
       if (inside<THREADS>(i, cols)) {

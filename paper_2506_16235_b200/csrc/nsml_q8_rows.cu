@@ -78,7 +78,8 @@ k_q8_pack(const typename Elem<DTYPE>::type* __restrict__ x, int64_t rows, int co
 
 // ---- restore ---------------------------------------------------------------------------------------------------------
 // A block takes kSpan columns of a row; narrow rows several at a time.  16384 x 8192 to bfloat16: 61 us, 6.6 TB/s; to float32
-// 8192 x 4096 37 us (a thread's 32 bytes are two stores).
+// 16384 x 2048 27 us, 6.2 TB/s (a thread's 32 bytes in two stores of 16: 38 us).  Rows off 16-byte boundaries: 16383 x 2047 23
+// and 36 us.
 constexpr int kSpan = 8192;
 
 template <int DTYPE, bool VEC, int THREADS>
