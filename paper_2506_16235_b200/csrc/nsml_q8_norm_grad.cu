@@ -48,15 +48,18 @@ __device__ __forceinline__ void copy_async(void* to, const void* from) {
   else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
 
-// Where a thread's chunks of the next row wait: two sets of dy, h (or codes) and dh.
+// Where a thread's chunks of the next row wait: two sets of dy, h (or codes) and dh; one where two do not fit, which is filled
+// again as soon as a chunk has been read for the last time (7056 x 9680 float32 with dh 401 us without, 275 with).
 template <int DTYPE, bool VEC, int THREADS, int CHUNKS>
 struct GradStage {
   static constexpr int kPiece = sizeof(Raw8<DTYPE, true>);
   static constexpr size_t kSet = (size_t)3 * CHUNKS * kPiece * grad_block<THREADS>();
-  static constexpr bool kAhead = VEC && 2 * kSet * (THREADS <= kGradBlock ? 2 : 1) <= 200 * 1024;  // (of two blocks, where an SM has two)
+  static constexpr size_t kRoom = 200 * 1024 / (THREADS <= kGradBlock ? 2 : 1);  // (of two blocks, where an SM has two)
+  static constexpr int kSets = !VEC || kSet > kRoom ? 0 : 2 * kSet <= kRoom ? 2 : 1;
+  static constexpr bool kAhead = kSets != 0;
   static constexpr size_t kSum = THREADS < kGradBlock ? (size_t)kGradBlock * CHUNKS * 32 : 0;       // the rows' parts of dweight, in the end
-  static constexpr size_t kSmem = kAhead ? 2 * kSet : kSum;
-  static_assert(!kAhead || 2 * kSet >= kSum, "");
+  static constexpr size_t kSmem = kAhead ? kSets * kSet : kSum;
+  static_assert(!kAhead || kSets * kSet >= kSum, "");
 };
 
 // KEEP: the weight has the rows' type, and a thread keeps its part in registers, as it is in memory (read from L1 for every row:
@@ -93,24 +96,22 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
   auto place = [&](int set, int o, int i) {
     return reinterpret_cast<unsigned char*>(stage) + set * G::kSet + ((size_t)(o * CHUNKS + i) * kBlock + threadIdx.x) * G::kPiece;
   };
+  auto chunk_ahead = [&](int set, int64_t at, int i) {
+    const unsigned int c = column<VEC, THREADS>(lane, i, 0);
+    if (at >= a.rows || c >= (unsigned int)a.cols) return;
+    const T *dy = static_cast<const T*>(a.dy) + at * a.ldy, *h = static_cast<const T*>(a.h) + at * a.ldh, *dh = static_cast<const T*>(a.dh) + at * a.lddh;
+#pragma unroll
+    for (int k = 0; k < G::kPiece; k += 16) {
+      copy_async<16>(place(set, 0, i) + k, reinterpret_cast<const char*>(dy + c) + k);
+      if constexpr (!PACKED) copy_async<16>(place(set, 1, i) + k, reinterpret_cast<const char*>(h + c) + k);
+      if (a.dh != nullptr) copy_async<16>(place(set, 2, i) + k, reinterpret_cast<const char*>(dh + c) + k);
+    }
+    if constexpr (PACKED) copy_async<8>(place(set, 1, i), a.codes + at * a.ldq + c);
+  };
   auto ahead = [&](int set, int64_t at) {
     if constexpr (G::kAhead) {
-      if (at < a.rows) {
-        const T *dy = static_cast<const T*>(a.dy) + at * a.ldy, *h = static_cast<const T*>(a.h) + at * a.ldh, *dh = static_cast<const T*>(a.dh) + at * a.lddh;
-        const int8_t* codes = a.codes + at * a.ldq;
 #pragma unroll
-        for (int i = 0; i < CHUNKS; ++i) {
-          const unsigned int c = column<VEC, THREADS>(lane, i, 0);
-          if (c >= (unsigned int)a.cols) continue;
-#pragma unroll
-          for (int k = 0; k < G::kPiece; k += 16) {
-            copy_async<16>(place(set, 0, i) + k, reinterpret_cast<const char*>(dy + c) + k);
-            if constexpr (!PACKED) copy_async<16>(place(set, 1, i) + k, reinterpret_cast<const char*>(h + c) + k);
-            if (a.dh != nullptr) copy_async<16>(place(set, 2, i) + k, reinterpret_cast<const char*>(dh + c) + k);
-          }
-          if constexpr (PACKED) copy_async<8>(place(set, 1, i), codes + c);
-        }
-      }
+      for (int i = 0; i < CHUNKS; ++i) chunk_ahead(set, at, i);
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
   };
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i)
       if (column<VEC, THREADS>(lane, i, 0) >= (unsigned int)a.cols)
-        for (int k = 0; k < 6 * G::kPiece; k += 16) *reinterpret_cast<uint4*>(place(k / (3 * G::kPiece), k / G::kPiece % 3, i) + k % G::kPiece) = make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < 3 * G::kSets * G::kPiece; k += 16) *reinterpret_cast<uint4*>(place(k / (3 * G::kPiece), k / G::kPiece % 3, i) + k % G::kPiece) = make_uint4(0, 0, 0, 0);
   }
   // rows that cannot be copied 16 bytes at a time: the next one is loaded into registers meanwhile, where they suffice
   constexpr bool kNext = !G::kAhead && THREADS <= 512;
@@ -145,14 +146,14 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
   ahead(0, row);
   if constexpr (kNext) load(row, next);
   for (int64_t turn = 0; turn < turns; ++turn, row += step) {
-    const int set = (int)(turn & 1), end = row < a.rows ? a.cols : 0;
+    const int sums_at = (int)(turn & 1), set = G::kSets == 2 ? sums_at : 0, end = row < a.rows ? a.cols : 0;
     const float rstd = rstd_next, factor = __fmul_rn(factor_next, rstd);
     Raw8<DTYPE, VEC, true> dy[CHUNKS], dh[CHUNKS], h[PACKED ? 1 : CHUNKS];
     RawCodes8<VEC, true> codes[PACKED ? CHUNKS : 1];
-    ahead(set ^ 1, row + step);
+    if constexpr (G::kSets == 2) ahead(set ^ 1, row + step);
     scalars(row + step, rstd_next, factor_next);
     if constexpr (G::kAhead) {
-      asm volatile("cp.async.wait_group 1;" ::: "memory");
+      asm volatile("cp.async.wait_group %0;" ::"n"(G::kSets - 1) : "memory");
     } else {
       if constexpr (!kNext) load(row, next);
 #pragma unroll
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
 #pragma unroll
     for (int d = (THREADS < 32 ? THREADS : 32) / 2; d; d >>= 1) dot = __fadd_rn(dot, __shfl_xor_sync(0xFFFFFFFFu, dot, d));
     if constexpr (THREADS > 32) {  // (two sets, so that one step of the row's warps per turn is enough)
-      float* const sums = shared[set][team];
+      float* const sums = shared[sums_at][team];
       if ((threadIdx.x & 31) == 0) sums[lane >> 5] = dot;
       if constexpr (kTeams > 1) asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(THREADS) : "memory");
       else __syncthreads();
@@ -237,7 +238,9 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
         g[j] = a.dh != nullptr ? __fmaf_rn(u, rstd, d[j]) : __fmul_rn(u, rstd);
       }
       store8<DTYPE, VEC, THREADS>(static_cast<T*>(a.dx) + row * a.lddx, lane, i, end, g);
+      if constexpr (G::kSets == 1) chunk_ahead(0, row + step, i);  // (behind the store, which has used all that was read there)
     }
+    if constexpr (G::kSets == 1) asm volatile("cp.async.commit_group;" ::: "memory");
   }
   if (a.partial == nullptr) return;
   float* const to = a.partial + (int64_t)blockIdx.x * a.cols;
