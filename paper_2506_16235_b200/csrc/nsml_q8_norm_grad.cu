@@ -127,6 +127,9 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
   }
   // rows that cannot be copied 16 bytes at a time: the next one is loaded into registers meanwhile, where they suffice
   constexpr bool kNext = !G::kAhead && THREADS <= 512;
+  // the widest of them are read again (from L2) instead: several chunks of a row in registers are too many for 1024 threads
+  // (7056 x 9681 bfloat16 with dh 600 us with four, 364 with two, 275 read again)
+  constexpr bool kAgain = !G::kAhead && CHUNKS > 1 && THREADS == 1024;
   struct {
     Raw8<DTYPE, VEC, true> dy[CHUNKS], dh[CHUNKS], h[PACKED ? 1 : CHUNKS];
     RawCodes8<VEC, true> codes[PACKED ? CHUNKS : 1];
@@ -154,7 +157,7 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
     scalars(row + step, rstd_next, factor_next);
     if constexpr (G::kAhead) {
       asm volatile("cp.async.wait_group %0;" ::"n"(G::kSets - 1) : "memory");
-    } else {
+    } else if constexpr (!kAgain) {
       if constexpr (!kNext) load(row, next);
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
@@ -166,7 +169,12 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
       if constexpr (kNext) load(row + step, next);
     }
     auto fetched = [&](int o, int i, const Raw8<DTYPE, VEC, true>& direct, float (&v)[8]) {
-      if constexpr (G::kAhead) {
+      if constexpr (kAgain) {
+        const T* from = static_cast<const T*>(o == 0 ? a.dy : o == 1 ? a.h : a.dh) + row * (o == 0 ? a.ldy : o == 1 ? a.ldh : a.lddh);
+        Raw8<DTYPE, VEC, true> x;
+        x.template load<THREADS>(from, lane, i, end);
+        x.widen(v);
+      } else if constexpr (G::kAhead) {
         const uint4* p = reinterpret_cast<const uint4*>(place(set, o, i));
         Raw8<DTYPE, VEC> x;
         x.set(0, p[0]);
@@ -183,6 +191,8 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
           const uint2 x = *reinterpret_cast<const uint2*>(place(set, 1, i));
           codes[i].w[0] = x.x;
           codes[i].w[1] = x.y;
+        } else if constexpr (kAgain) {
+          codes[i].template load<THREADS>(a.codes + row * a.ldq, lane, i, end);
         }
         codes[i].numbers(v);
       }
@@ -214,7 +224,7 @@ __global__ void __launch_bounds__(grad_block<THREADS>(), THREADS <= kGradBlock ?
 #pragma unroll
       for (int k = 1; k < kWarps; ++k) dot = __fadd_rn(dot, sums[k]);
     }
-    if constexpr (!G::kAhead) {
+    if constexpr (!G::kAhead && !kAgain) {
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
         forget(dy[i]);
@@ -333,7 +343,11 @@ static int norm_grad_rows(const NormGradArgs& a, cudaStream_t st) {
   using std::integral_constant;
   constexpr int C = grad_chunks(DTYPE, VEC), kLeast = 128 / (8 * C);  // 4, 8 or 16
   const int threads = grad_threads(a.cols, DTYPE, VEC);
-  if (threads == 1024 && a.cols > 8192 * C) return go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+  if (threads == 1024 && a.cols > 8192 * C) {
+    if constexpr (C == 1)  // (four chunks do not fit into the registers)
+      if (a.cols <= 16384) return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    return go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+  }
   if (threads == kLeast) return go(integral_constant<int, kLeast>{}, integral_constant<int, C>{});
   switch (threads) {
     case 16: if constexpr (kLeast == 4) return go(integral_constant<int, 16>{}, integral_constant<int, C>{});

@@ -453,3 +453,24 @@ def test_a_layers_step_runs_and_is_captured_and_replayed():
         fresh = torch.zeros_like(bucket)
         y, dx = layer_step(static["x"].clone(), residual, wn, w, static["dy"].clone(), fresh, ws)
         assert torch.equal(y, out[0]) and torch.equal(dx, out[1]) and torch.equal(fresh, static["bucket"])
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [2047, 8200, 9681, 12288, 16390, 20480, 32768])
+def test_norm_backward_several_wide_rows_per_block(cols, dtype, packed):
+    rows = 310  # (three turns of a block that has an SM to itself)
+    weight = (1.0 + 0.1 * torch.randn(cols, generator=torch.Generator().manual_seed(1))).to(dtype).cuda()
+    h, dy, dh = rand(rows, cols, dtype, 1), rand(rows, cols, dtype, 2, 1e-3), rand(rows, cols, dtype, 3, 1e-3)
+    rstd = nsml.nsml_q8_rms_norm(h, weight)[2]
+    codes, scales = nsml.nsml_q8_pack(h)
+    kept = f64(h) if not packed else plain.unpack(codes_of(codes), f64(scales))
+    rows_kept = dict(codes=codes, scales=scales) if packed else dict(h=h)
+    dx, dweight = nsml.nsml_q8_rms_norm_backward(dy, weight, rstd, dh=dh, **rows_kept)
+    want_dx, want_dw = plain.rms_norm_backward(f64(dy), kept, f64(rstd), f64(weight), f64(dh))
+    tol, tol_w = norm_grad_tolerance(f64(dy), kept, f64(rstd), f64(weight), f64(dh), want_dx, dtype, rows)
+    assert np.all(np.abs(f64(dx) - want_dx) <= tol)
+    assert np.all(np.abs(f64(dweight) - want_dw) <= tol_w)
+    for into in (dy.clone(), dh.clone()):  # in place
+        args = (into, dh) if torch.equal(into, dy) else (dy, into)
+        assert torch.equal(nsml.nsml_q8_rms_norm_backward(args[0], weight, rstd, dh=args[1], dx=into, **rows_kept)[0], dx)
