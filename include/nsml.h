@@ -573,6 +573,15 @@ int nsml_last_status(const void* workspace, void* stream, int* status_out);
  * workspace stays usable: every call clears its control block first. */
 int nsml_selftest_bounded_wait(void* workspace, size_t workspace_bytes, int max_polls, void* stream);
 
+/* Self-test of the bounded waits inside the 8-bit products, whose warps wait as
+ * a whole for barriers in shared memory.  Enqueues a kernel of one warp whose
+ * first `lanes` lanes (0 .. 32) wait for a barrier that nobody arrives at (a
+ * millisecond) while the others' is complete.  If any lane gives up, all of
+ * them do: the status word of `workspace` (256-byte aligned, >= 256 bytes) reads
+ * NSML_ERR_TIMEOUT afterwards, with lanes = 0 NSML_OK (and NSML_ERR_INTERNAL if
+ * the lanes disagreed). */
+int nsml_selftest_q8_bounded_wait(void* workspace, size_t workspace_bytes, int lanes, void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* nsml_strerror(int status);
 

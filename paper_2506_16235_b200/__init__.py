@@ -135,6 +135,7 @@ def _load() -> ctypes.CDLL:
         "nsml_q8_matmul_grad_input": (ci, [vp, i64, vp, i64, vp, i64, i64, i64, vp, i64, ci, vp, sz, vp]),
         "nsml_q8_matmul_grad_weight": (ci, [vp, i64, vp, i64, vp, i64, i64, i64, vp, i64, ci, ci, vp, sz, vp]),
         "nsml_selftest_bounded_wait": (ci, [vp, sz, ci, vp]),
+        "nsml_selftest_q8_bounded_wait": (ci, [vp, sz, ci, vp]),
         "nsml_last_status": (ci, [vp, vp, ctypes.POINTER(ci)]),
         "nsml_strerror": (ctypes.c_char_p, [ci]),
         "nsml_kernel_count": (ci, []),

@@ -81,21 +81,28 @@ __device__ __forceinline__ bool bar_try_at(uint32_t bar, uint32_t parity) {
   return done != 0;
 }
 // false: the wait ran out (here or, as `failed` says, elsewhere in the block)
-template <bool CLUSTER>
+template <bool CLUSTER, unsigned long long LIMIT>
 __device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile int* failed) {
   const unsigned long long from = now_ns();
   while (true) {
     for (int i = 0; i < 64; ++i)
       if (bar_try_at<CLUSTER>(bar, parity)) return true;
-    if (*failed != 0 || now_ns() - from > kWaitNs) {
+    if (*failed != 0 || now_ns() - from > LIMIT) {
       *failed = 1;
       return false;
     }
   }
 }
-template <bool CLUSTER = false>
+// For one thread.
+template <bool CLUSTER = false, unsigned long long LIMIT = kWaitNs>
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
-  return bar_try_at<CLUSTER>(bar, parity) || bar_wait_slow<CLUSTER>(bar, parity, failed);
+  return bar_try_at<CLUSTER>(bar, parity) || bar_wait_slow<CLUSTER, LIMIT>(bar, parity, failed);
+}
+// For a whole warp, which then goes on as one (tcgen05.ld and .st want all of its lanes): the lanes poll on their own, and one
+// may give up just as the barrier completes for another, so they agree on what came of it.  False if any lane gave up.
+template <unsigned long long LIMIT = kWaitNs>
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
+  return __all_sync(0xFFFFFFFFu, bar_wait<false, LIMIT>(bar, parity, failed));
 }
 __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {  // the same place in another block of the cluster
   uint32_t r;
@@ -108,6 +115,7 @@ __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();  // (aligned: the warp's lanes arrive together, one that has been on its own among them)
   asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
@@ -536,7 +544,7 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
       tile_at(t, high, g.tiles_m, g.tiles_n, m, n);
       for (int piece = from; piece < to; piece += g.piece, ++unit) {
         const uint32_t buffer = unit & 1, acc = tmem + buffer * S::kTile + ((uint32_t)quarter << 21);
-        if (!(ok = bar_wait(acc_full + 8 * buffer, (unit >> 1) & 1, &failed))) break;
+        if (!(ok = warp_wait(acc_full + 8 * buffer, (unit >> 1) & 1, &failed))) break;
         tc_fence_after();
         auto release = [&] {  // the accumulator has been read
           tc_fence_before();
@@ -545,6 +553,7 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
             if constexpr (PAIR) bar_arrive_cluster(in_block(acc_empty + 8 * buffer, 0));
             else bar_arrive(acc_empty + 8 * buffer);
           }
+          __syncwarp();  // (the next access to TMEM is the whole warp's again)
         };
         if constexpr (PAIR) {
           unsigned char* const stage = out + (warp - 4) * 4096;  // 32 rows of 128 bytes, pieces of 16 swizzled
@@ -656,7 +665,7 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
       const int64_t mine = first < tiles ? (tiles - first + stride - 1) / stride : 0, total = mine * (to - from);
       for (int64_t it = (warp - S::kFirstRestorer) / kTurn; it < total; it += kTurns) {
         const uint32_t s = (uint32_t)(it % S::kCodes), w = (uint32_t)(it % S::kWides);
-        if (!bar_wait(codes_full + 8 * s, (uint32_t)(it / S::kCodes) & 1, &failed)) break;
+        if (!warp_wait(codes_full + 8 * s, (uint32_t)(it / S::kCodes) & 1, &failed)) break;
         const unsigned char* codes = ring_ptr + S::kCodeAt + s * S::kCode;
         const float* scales = reinterpret_cast<const float*>(codes + 128 * 64) + g.scale_shift;
         unsigned char* dst = ring_ptr + S::kWideAt + w * S::kWide + (sub >> 2) * 8192;
@@ -672,7 +681,7 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
         }
         __syncwarp();
         if (lane == 0) bar_arrive(codes_empty + 8 * s);  // (they are in registers)
-        if (!bar_wait(wide_empty + 8 * w, ((uint32_t)(it / S::kWides) & 1) ^ 1, &failed)) break;
+        if (!warp_wait(wide_empty + 8 * w, ((uint32_t)(it / S::kWides) & 1) ^ 1, &failed)) break;
         auto convert = [&](auto kind) {
 #pragma unroll
           for (int i = 0; i < kRows / 4; ++i) {
@@ -731,6 +740,24 @@ k_q8_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUt
     }
     cluster_sync();  // no block leaves while another reads its part
   }
+}
+
+// The waits' limit reached on purpose: one warp, whose first `lanes` lanes wait for a barrier that nobody arrives at (a millisecond)
+// and the others for one that is complete.  The lanes have to end up with one answer, and together.
+__global__ void __launch_bounds__(32) k_q8_wait_probe(int lanes, int* status) {
+  __shared__ alignas(8) uint64_t bars[2];
+  __shared__ int failed;
+  const uint32_t never = smem_addr(bars), done = never + 8;
+  if (threadIdx.x == 0) {
+    bar_init(never, 1);
+    bar_init(done, 1);
+    failed = 0;
+    bar_arrive(done);
+  }
+  __syncwarp();
+  const bool ok = warp_wait<1000000ull>((int)threadIdx.x < lanes ? never : done, 0, &failed);
+  const uint32_t agreed = __ballot_sync(0xFFFFFFFFu, ok);
+  if (threadIdx.x == 0) *status = agreed == 0 ? NSML_ERR_TIMEOUT : agreed == 0xFFFFFFFFu ? NSML_OK : NSML_ERR_INTERNAL;
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
@@ -977,6 +1004,13 @@ int nsml_q8_matmul_grad_weight(const void* dy, int64_t ldy, const int8_t* a, int
   CUtensorMap map_a, map_b, map_scales;
   if (!scales_map(&map_scales, a_scales, m, &g.scale_shift) || !tensor_map(&map_a, dy, false, m, n, ldy, 64, 64, true) || !tensor_map(&map_b, a, true, m, k, lda, 128, 64, false)) return NSML_ERR_CUDA;
   return launch_gemm<kGradWeight>(map_a, map_b, map_scales, g, *dev, st);
+}
+
+int nsml_selftest_q8_bounded_wait(void* workspace, size_t workspace_bytes, int lanes, void* stream) {
+  if (workspace == nullptr || !aligned(workspace, 256) || lanes < 0 || lanes > 32) return NSML_ERR_ARG;
+  if (workspace_bytes < NSML_Q8_MATMUL_WORKSPACE_BYTES) return NSML_ERR_CAPACITY;
+  k_q8_wait_probe<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>(lanes, static_cast<int*>(workspace));
+  return cudaGetLastError() == cudaSuccess ? NSML_OK : NSML_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -1,0 +1,14 @@
+"""More refusals of the 8-bit operators' entry points, decided before anything is launched (no GPU)."""
+import ctypes
+
+import paper_2506_16235_b200 as nsml
+
+lib, ARG, CAPACITY = nsml.lib, nsml.NSML_ERR_ARG, nsml.NSML_ERR_CAPACITY
+BUFFER = (ctypes.c_char * 8192)()
+AT = (ctypes.addressof(BUFFER) + 255) // 256 * 256  # an aligned address that stands in for device memory
+
+
+def test_selftest_of_the_waits_refuses():
+    wait = lib.nsml_selftest_q8_bounded_wait
+    assert wait(None, 256, 1, None) == wait(AT + 16, 256, 1, None) == wait(AT, 256, -1, None) == wait(AT, 256, 33, None) == ARG
+    assert wait(AT, 255, 1, None) == CAPACITY
