@@ -198,12 +198,28 @@ class NormLinear:
     def backward(self, dy: torch.Tensor, dh: torch.Tensor = None, zero_first: bool = True) -> torch.Tensor:
         """dy [m, n] (bfloat16, n a multiple of 8): writes (zero_first=False: adds) the weights' gradients and returns the
         gradient of x and residual (bfloat16), dh (a gradient that reaches h past the norm) included.  Frees what the forward
-        pass kept."""
+        pass kept; a call that is refused has written nothing and frees nothing."""
         if self.kept is None:
             raise RuntimeError("backward() without a forward() before it")
-        (rows, scales, rstd, (h_codes, h_scales)), self.kept = self.kept, None
-        nsml = self.nsml
+        rows, scales, rstd, (h_codes, h_scales) = self.kept
+        # whatever a call below would refuse is refused here, before the first of them has written anything
+        self._check_rows(dy, "dy", (rows.shape[0], self.codes.shape[0]), torch.bfloat16)
+        if rows.shape[0] and (dy.data_ptr() % 16 or (rows.shape[0] > 1 and dy.stride(0) % 8)):
+            raise ValueError("dy must have its rows on 16-byte boundaries")
+        if dh is not None:
+            self._check_rows(dh, "dh", rows.shape, torch.bfloat16)
+        nsml, dnormed = self.nsml, torch.empty(rows.shape, dtype=torch.bfloat16, device=rows.device)
         nsml.nsml_q8_matmul_grad_weight(dy, rows, scales, dw=self.grad_weight, zero_first=zero_first, workspace=self.workspaces[1])
-        dnormed = nsml.nsml_q8_matmul_grad_input(dy, self.codes, self.scales, workspace=self.workspaces[2])
-        return nsml.nsml_q8_rms_norm_backward(dnormed, self.norm_weight, rstd, codes=h_codes, scales=h_scales, dh=dh, dx=dnormed,
-                                              dweight=self.grad_norm_weight, zero_first=zero_first, workspace=self.norm_workspace)[0]
+        nsml.nsml_q8_matmul_grad_input(dy, self.codes, self.scales, dx=dnormed, workspace=self.workspaces[2])
+        nsml.nsml_q8_rms_norm_backward(dnormed, self.norm_weight, rstd, codes=h_codes, scales=h_scales, dh=dh, dx=dnormed,
+                                       dweight=self.grad_norm_weight, zero_first=zero_first, workspace=self.norm_workspace)
+        self.kept = None
+        return dnormed
+
+    def _check_rows(self, t: torch.Tensor, what: str, shape, dtype) -> None:
+        if t.dtype is not dtype:
+            raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
+        if tuple(t.shape) != tuple(shape) or t.device != self.codes.device:
+            raise ValueError(f"{what} must have shape {tuple(shape)} and be on {self.codes.device}")
+        if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
