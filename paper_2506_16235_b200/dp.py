@@ -196,19 +196,28 @@ class NormLinear:
         return self.nsml.nsml_q8_matmul(rows, scales, self.codes, self.scales, dtype=x.dtype, workspace=self.workspaces[0]), h
 
     def backward(self, dy: torch.Tensor, dh: torch.Tensor = None, zero_first: bool = True) -> torch.Tensor:
-        """dy [m, n] (bfloat16, n a multiple of 8): writes (zero_first=False: adds) the weights' gradients and returns the
-        gradient of x and residual (bfloat16), dh (a gradient that reaches h past the norm) included.  Frees what the forward
-        pass kept; a call that is refused has written nothing and frees nothing."""
+        """dy [m, n] (of y's type, bfloat16 or float32, contiguous rows): writes (zero_first=False: adds) the weights' gradients
+        and returns the gradient of x and residual, dh (a gradient that reaches h past the norm) included.  dh and the result
+        have dy's type.  The products take bfloat16 rows on 16-byte boundaries: a dy that is not that (float32, which is rounded
+        to bfloat16; an n that is no multiple of 8) is copied first.  Frees what the forward pass kept; a call that is refused
+        has written nothing and frees nothing."""
         if self.kept is None:
             raise RuntimeError("backward() without a forward() before it")
         rows, scales, rstd, (h_codes, h_scales) = self.kept
+        m, n = rows.shape[0], self.codes.shape[0]
         # whatever a call below would refuse is refused here, before the first of them has written anything
-        self._check_rows(dy, "dy", (rows.shape[0], self.codes.shape[0]), torch.bfloat16)
-        if rows.shape[0] and (dy.data_ptr() % 16 or (rows.shape[0] > 1 and dy.stride(0) % 8)):
-            raise ValueError("dy must have its rows on 16-byte boundaries")
-        if dh is not None:
-            self._check_rows(dh, "dh", rows.shape, torch.bfloat16)
-        nsml, dnormed = self.nsml, torch.empty(rows.shape, dtype=torch.bfloat16, device=rows.device)
+        if dy.dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError(f"dy must be bfloat16 or float32, not {dy.dtype}")
+        for t, what, shape in ((dy, "dy", (m, n)), (dh, "dh", rows.shape)):
+            if t is None:
+                continue
+            if t.dtype is not dy.dtype:
+                raise TypeError(f"{what} must be {dy.dtype}, not {t.dtype}")
+            if tuple(t.shape) != tuple(shape) or t.device != self.codes.device:
+                raise ValueError(f"{what} must have shape {tuple(shape)} and be on {self.codes.device}")
+            if (t.shape[1] > 1 and t.stride(1) != 1) or (m > 1 and t.stride(0) < t.shape[1]):
+                raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
+        nsml, dnormed, dy = self.nsml, torch.empty(rows.shape, dtype=dy.dtype, device=rows.device), self._for_products(dy)
         nsml.nsml_q8_matmul_grad_weight(dy, rows, scales, dw=self.grad_weight, zero_first=zero_first, workspace=self.workspaces[1])
         nsml.nsml_q8_matmul_grad_input(dy, self.codes, self.scales, dx=dnormed, workspace=self.workspaces[2])
         nsml.nsml_q8_rms_norm_backward(dnormed, self.norm_weight, rstd, codes=h_codes, scales=h_scales, dh=dh, dx=dnormed,
@@ -216,10 +225,10 @@ class NormLinear:
         self.kept = None
         return dnormed
 
-    def _check_rows(self, t: torch.Tensor, what: str, shape, dtype) -> None:
-        if t.dtype is not dtype:
-            raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
-        if tuple(t.shape) != tuple(shape) or t.device != self.codes.device:
-            raise ValueError(f"{what} must have shape {tuple(shape)} and be on {self.codes.device}")
-        if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-            raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
+    @staticmethod
+    def _for_products(dy: torch.Tensor) -> torch.Tensor:
+        """dy (contiguous rows) as the products' gradients take it: bfloat16, rows on 16-byte boundaries."""
+        m, n = dy.shape
+        if dy.dtype is torch.bfloat16 and dy.data_ptr() % 16 == 0 and (m <= 1 or dy.stride(0) % 8 == 0):
+            return dy
+        return torch.empty(m, (n + 7) // 8 * 8, dtype=torch.bfloat16, device=dy.device)[:, :n].copy_(dy.detach())

@@ -60,3 +60,15 @@ def test_what_was_kept_outlives_a_call_that_fails(fail_at):
     block.nsml = Calls()
     block.backward(bf16(M, N))
     assert block.kept is None
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,pad,lead", [(16, 0, 0), (16, 8, 0), (13, 0, 0), (16, 4, 0), (16, 0, 3), (1, 0, 1)])
+def test_the_products_are_given_rows_on_16_byte_boundaries(n, pad, lead, dtype):
+    buf = torch.randn(lead + 5 * (n + pad), generator=torch.Generator().manual_seed(1)).to(dtype)
+    dy = buf[lead:].view(5, n + pad)[:, :n]
+    got = dp.NormLinear._for_products(dy)
+    assert got.dtype is torch.bfloat16 and torch.equal(got, dy.bfloat16()) and got.data_ptr() % 16 == 0 and got.stride(0) % 8 == 0
+    assert (got is dy) == (dtype is torch.bfloat16 and dy.data_ptr() % 16 == 0 and dy.stride(0) % 8 == 0)
+    with_graph = dy.float().requires_grad_()
+    assert not dp.NormLinear._for_products(with_graph).requires_grad
