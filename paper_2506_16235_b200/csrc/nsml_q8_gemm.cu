@@ -916,11 +916,24 @@ static bool valid_operand(const void* p, int64_t rows, int64_t cols, int64_t ld)
 static bool valid_gradient(const void* p, int64_t rows, int64_t cols, int64_t ld) {
   return p != nullptr && aligned(p, 16) && (rows <= 1 || (ld >= cols && ld % 8 == 0 && ld < ((int64_t)1 << 39)));
 }
+// A call without tokens: nothing to compute, but the workspace's status is this call's.  (An address that CUDA does not know, as
+// every one is on a machine without a device, is left alone.)
+static int no_tokens(void* workspace, cudaStream_t st) {
+  cudaPointerAttributes where;
+  if (cudaPointerGetAttributes(&where, workspace) != cudaSuccess || where.type == cudaMemoryTypeUnregistered) {
+    cudaGetLastError();
+    return NSML_OK;
+  }
+  return cudaMemsetAsync(workspace, 0, NSML_Q8_MATMUL_WORKSPACE_BYTES, st) == cudaSuccess ? NSML_OK : cuda_error();
+}
+static int check_workspace(const void* workspace, size_t workspace_bytes) {
+  if (workspace == nullptr || !aligned(workspace, 256)) return NSML_ERR_ARG;
+  return workspace_bytes < NSML_Q8_MATMUL_WORKSPACE_BYTES ? NSML_ERR_CAPACITY : NSML_OK;
+}
 static int check_out(const void* out, int64_t rows, int64_t cols, int64_t ldo, int dtype, const void* workspace, size_t workspace_bytes) {
   if (dtype != NSML_F32 && dtype != NSML_BF16) return NSML_ERR_ARG;
   if (out == nullptr || !aligned(out, dtype == NSML_F32 ? 4 : 2) || (rows > 1 && ldo < cols)) return NSML_ERR_ARG;
-  if (workspace == nullptr || !aligned(workspace, 256)) return NSML_ERR_ARG;
-  return workspace_bytes < NSML_Q8_MATMUL_WORKSPACE_BYTES ? NSML_ERR_CAPACITY : NSML_OK;
+  return check_workspace(workspace, workspace_bytes);
 }
 static GemmArgs result(void* out, int64_t rows, int64_t cols, int64_t ldo, int dtype, bool add, void* workspace) {
   GemmArgs g = {};
@@ -947,10 +960,11 @@ extern "C" {
 int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const int8_t* b, int64_t ldb, const float* b_scales, int64_t m,
                    int64_t n, int64_t k, void* out, int64_t ldo, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (!valid_size(m) || !valid_size(n) || n < 1 || k < 1 || k > NSML_Q8_MAX_DEPTH) return NSML_ERR_ARG;
-  if (m == 0) return NSML_OK;
+  int rc = check_workspace(workspace, workspace_bytes);
+  if (m == 0) return rc == NSML_OK ? no_tokens(workspace, static_cast<cudaStream_t>(stream)) : rc;
   if (!valid_operand(a, m, k, lda) || !valid_operand(b, n, k, ldb) || a_scales == nullptr || !aligned(a_scales, 4) || b_scales == nullptr || !aligned(b_scales, 4))
     return NSML_ERR_ARG;
-  int rc = check_out(out, m, n, ldo, dtype, workspace, workspace_bytes);
+  rc = check_out(out, m, n, ldo, dtype, workspace, workspace_bytes);
   if (rc != NSML_OK) return rc;
   if (m <= kMaxTokens)
     return launch_tokens(a, lda, a_scales, b, ldb, b_scales, (int)m, n, (int)k, out, ldo, dtype == NSML_BF16, static_cast<int*>(workspace),
@@ -969,9 +983,10 @@ int nsml_q8_matmul(const int8_t* a, int64_t lda, const float* a_scales, const in
 int nsml_q8_matmul_grad_input(const void* dy, int64_t ldy, const int8_t* b, int64_t ldb, const float* b_scales, int64_t m, int64_t n, int64_t k,
                               void* dx, int64_t lddx, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (!valid_size(m) || !valid_size(n) || !valid_size(k) || n < 1 || k < 1 || n > NSML_Q8_MAX_GRAD_DEPTH) return NSML_ERR_ARG;
-  if (m == 0) return NSML_OK;
+  int rc = check_workspace(workspace, workspace_bytes);
+  if (m == 0) return rc == NSML_OK ? no_tokens(workspace, static_cast<cudaStream_t>(stream)) : rc;
   if (!valid_gradient(dy, m, n, ldy) || !valid_operand(b, n, k, ldb) || b_scales == nullptr || !aligned(b_scales, 4)) return NSML_ERR_ARG;
-  int rc = check_out(dx, m, k, lddx, dtype, workspace, workspace_bytes);
+  rc = check_out(dx, m, k, lddx, dtype, workspace, workspace_bytes);
   if (rc != NSML_OK) return rc;
   const GemmDevice* dev = nullptr;
   if ((rc = gemm_device(&dev)) != NSML_OK) return rc;
@@ -991,7 +1006,7 @@ int nsml_q8_matmul_grad_weight(const void* dy, int64_t ldy, const int8_t* a, int
   if (rc != NSML_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (m == 0) {  // an empty sum
-    if (cudaMemsetAsync(workspace, 0, 256, st) != cudaSuccess) return cuda_error();
+    if ((rc = no_tokens(workspace, st)) != NSML_OK) return rc;
     const size_t size = dtype == NSML_F32 ? 4 : 2;
     if (zero_first && cudaMemset2DAsync(dw, (size_t)(n > 1 ? lddw : k) * size, 0, (size_t)k * size, (size_t)n, st) != cudaSuccess) return cuda_error();
     return NSML_OK;
