@@ -466,7 +466,8 @@ int nsml_decompress_accumulate_host(const void* const* payloads_host, const size
  * Sizes: rows and columns up to NSML_Q8_MAX_ROWS / NSML_Q8_MAX_COLS; zero rows
  * (tokens) are allowed and leave the outputs of rows alone; the status word of a
  * workspace is written all the same.  Every output is reproducible bit for bit
- * on a device.  Nothing synchronises; all calls can be captured into a graph.
+ * on a device.  Nothing synchronises; all calls can be captured into a graph, and
+ * run at the priority of `stream`.
  * ---------------------------------------------------------------------- */
 #define NSML_Q8_MAX_ROWS 2147483647LL
 #define NSML_Q8_MAX_COLS 2147483632LL

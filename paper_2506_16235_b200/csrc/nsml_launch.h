@@ -36,9 +36,10 @@ inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_
 
 int high_priority();  // the device's highest stream priority
 
+// priority: null leaves the stream's
 template <class... KArgs, class... Args>
-static cudaError_t launch_prio(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool cooperative,
-                               unsigned int cluster_x, bool high, bool dependent, Args... args) {
+static cudaError_t launch_at(const int* priority, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool cooperative,
+                             unsigned int cluster_x, bool dependent, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
@@ -46,9 +47,11 @@ static cudaError_t launch_prio(void (*kernel)(KArgs...), dim3 grid, dim3 block, 
   cfg.stream = st;
   cudaLaunchAttribute attr[4];
   unsigned int na = 0;
-  attr[na].id = cudaLaunchAttributePriority;
-  attr[na].val.priority = high ? high_priority() : 0;
-  ++na;
+  if (priority != nullptr) {
+    attr[na].id = cudaLaunchAttributePriority;
+    attr[na].val.priority = *priority;
+    ++na;
+  }
   if (cooperative) {
     attr[na].id = cudaLaunchAttributeCooperative;
     attr[na].val.cooperative = 1;
@@ -70,6 +73,20 @@ static cudaError_t launch_prio(void (*kernel)(KArgs...), dim3 grid, dim3 block, 
   cfg.attrs = attr;
   cfg.numAttrs = na;
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
+// The compression's kernels: a priority of their own, whatever the stream's (high: the device's highest, otherwise 0).
+template <class... KArgs, class... Args>
+static cudaError_t launch_prio(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool cooperative,
+                               unsigned int cluster_x, bool high, bool dependent, Args... args) {
+  const int priority = high ? high_priority() : 0;
+  return launch_at(&priority, kernel, grid, block, smem, st, cooperative, cluster_x, dependent, args...);
+}
+
+// The 8-bit operators' kernels: at the stream's priority, dependent.
+template <class... KArgs, class... Args>
+static cudaError_t launch_in_stream(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, unsigned int cluster_x, Args... args) {
+  return launch_at(nullptr, kernel, grid, block, smem, st, false, cluster_x, true, args...);
 }
 
 }  // namespace nsml

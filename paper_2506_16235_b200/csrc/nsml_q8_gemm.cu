@@ -899,11 +899,11 @@ static int launch_gemm(const CUtensorMap& map_a, const CUtensorMap& map_b, const
     auto* kernel = k_q8_gemm<MODE, true, false>;
     if constexpr (MODE != kForward)
       if (g.add || g.piece < g.steps) kernel = k_q8_gemm<MODE, true, true>;
-    e = launch_prio(kernel, dim3((unsigned int)(2 * (tiles < dev.pairs[1] ? tiles : dev.pairs[1]))), dim3(S::kThreads), S::kSmem, st, false, 2, false, true, map_a, map_b,
+    e = launch_in_stream(kernel, dim3((unsigned int)(2 * (tiles < dev.pairs[1] ? tiles : dev.pairs[1]))), dim3(S::kThreads), S::kSmem, st, 2, map_a, map_b,
                     map_scales, g);
   } else {
     using S = Shape<MODE, false>;
-    e = launch_prio(k_q8_gemm<MODE, false, false>, dim3((unsigned int)(tiles * form)), dim3(S::kThreads), S::kSmem, st, false, (unsigned int)form, false, true,
+    e = launch_in_stream(k_q8_gemm<MODE, false, false>, dim3((unsigned int)(tiles * form)), dim3(S::kThreads), S::kSmem, st, (unsigned int)form,
                     map_a, map_b, map_scales, g);
   }
   return e == cudaSuccess ? NSML_OK : cuda_error();

@@ -336,8 +336,8 @@ static int norm_grad_rows(const NormGradArgs& a, cudaStream_t st) {
       }
     }
     LaunchScope scope(K_Q8_NORM_GRAD, st);
-    e = launch_prio(k_q8_norm_grad<DTYPE, PACKED, VEC, KEEP, THREADS, CHUNKS>, dim3(grad_blocks(a.rows, a.cols, DTYPE, VEC)), dim3(grad_block<THREADS>()), smem, st, false,
-                    0, false, true, a);
+    e = launch_in_stream(k_q8_norm_grad<DTYPE, PACKED, VEC, KEEP, THREADS, CHUNKS>, dim3(grad_blocks(a.rows, a.cols, DTYPE, VEC)), dim3(grad_block<THREADS>()), smem, st,
+                         0, a);
     return e == cudaSuccess ? NSML_OK : cuda_error();
   };
   using std::integral_constant;
@@ -417,9 +417,9 @@ int nsml_q8_rms_norm_backward(const void* dy, int64_t ldy, const void* dh, int64
   }
   if (dweight != nullptr) {
     LaunchScope scope(K_Q8_NORM_WEIGHT, st);
-    const cudaError_t e = launch_prio(k_q8_norm_weight, dim3((unsigned int)((cols + 31) / 32)), dim3(1024), 0, st, false, 0, true, true,
-                                      static_cast<const float*>(table), grad_blocks(rows, cols, dtype, vec), cols, dweight,
-                                      dweight_dtype == NSML_BF16, zero_first != 0, static_cast<int*>(workspace));
+    const cudaError_t e = launch_in_stream(k_q8_norm_weight, dim3((unsigned int)((cols + 31) / 32)), dim3(1024), 0, st, 0,
+                                           static_cast<const float*>(table), grad_blocks(rows, cols, dtype, vec), cols, dweight,
+                                           dweight_dtype == NSML_BF16, zero_first != 0, static_cast<int*>(workspace));
     if (e != cudaSuccess) return cuda_error();
   }
   return NSML_OK;

@@ -232,7 +232,7 @@ static int pack_rows(const void* x, int64_t rows, int64_t cols, int64_t ldx, int
   return by_width(cols, [&](auto threads) {
     constexpr int THREADS = threads;
     LaunchScope scope(K_Q8_PACK, st);
-    const cudaError_t e = launch_prio(k_q8_pack<DTYPE, VEC, THREADS>, row_grid<THREADS>(rows), dim3(block_threads<THREADS>()), 0, st, false, 0, false, true,
+    const cudaError_t e = launch_in_stream(k_q8_pack<DTYPE, VEC, THREADS>, row_grid<THREADS>(rows), dim3(block_threads<THREADS>()), 0, st, 0,
                                       static_cast<const T*>(x), rows, (int)cols, ldx, codes, ldq, scales);
     return e == cudaSuccess ? NSML_OK : cuda_error();
   });
@@ -246,7 +246,7 @@ static int unpack_rows(const int8_t* codes, int64_t ldq, const float* scales, in
     const int64_t spans = (cols + kSpan - 1) / kSpan, blocks = spans * row_grid<THREADS>(rows).x;
     if (blocks > NSML_Q8_MAX_ROWS) return (int)NSML_ERR_ARG;
     LaunchScope scope(K_Q8_UNPACK, st);
-    const cudaError_t e = launch_prio(k_q8_unpack<DTYPE, VEC, THREADS>, dim3((unsigned int)blocks), dim3(block_threads<THREADS>()), 0, st, false, 0, false, true,
+    const cudaError_t e = launch_in_stream(k_q8_unpack<DTYPE, VEC, THREADS>, dim3((unsigned int)blocks), dim3(block_threads<THREADS>()), 0, st, 0,
                                       codes, ldq, scales, rows, (int)cols, static_cast<T*>(out), ldo, (unsigned int)spans);
     return e == cudaSuccess ? (int)NSML_OK : cuda_error();
   });
@@ -257,7 +257,7 @@ static int norm_rows(const NormArgs& a, cudaStream_t st) {
   return by_width(a.cols, [&](auto threads) {
     constexpr int THREADS = threads;
     LaunchScope scope(K_Q8_NORM, st);
-    const cudaError_t e = launch_prio(k_q8_norm<DTYPE, VEC, THREADS>, row_grid<THREADS>(a.rows), dim3(block_threads<THREADS>()), 0, st, false, 0, false, true, a);
+    const cudaError_t e = launch_in_stream(k_q8_norm<DTYPE, VEC, THREADS>, row_grid<THREADS>(a.rows), dim3(block_threads<THREADS>()), 0, st, 0, a);
     return e == cudaSuccess ? NSML_OK : cuda_error();
   });
 }

@@ -91,8 +91,8 @@ int launch_tokens(const int8_t* a, int64_t lda, const float* sa, const int8_t* b
   auto go = [&](auto tokens, auto split) {
     constexpr int M = tokens, SPLIT = split, per_block = kRows * kTokenWarps / SPLIT;
     LaunchScope scope(K_Q8_TOKENS, st);
-    const cudaError_t e = launch_prio(k_q8_tokens<M, SPLIT>, dim3((unsigned int)((n + per_block - 1) / per_block)), dim3(32 * kTokenWarps), 0, st, false, 0, false,
-                                      true, a, lda, sa, b, ldb, sb, m, n, k, out, ldo, bf16, status);
+    const cudaError_t e = launch_in_stream(k_q8_tokens<M, SPLIT>, dim3((unsigned int)((n + per_block - 1) / per_block)), dim3(32 * kTokenWarps), 0, st, 0,
+                                           a, lda, sa, b, ldb, sb, m, n, k, out, ldo, bf16, status);
     return e == cudaSuccess ? NSML_OK : cuda_error();
   };
   // enough warps to have the memory busy (some 2000), but not so many that a lane has nothing to read (512 codes per warp)
