@@ -207,8 +207,8 @@ __global__ void __launch_bounds__(block_threads<THREADS>()) k_q8_norm(const Norm
   }
 }
 
-// Threads for a row of up to `cols` columns: 32 columns (four chunks) each.
-template <class Launch>
+// Threads for a row of up to `cols` columns: 32 columns (four chunks) each.  MOST: no more of them than that.
+template <int MOST = 1024, class Launch>
 static int by_width(int64_t cols, Launch launch) {
   using std::integral_constant;
   if (cols <= 128) return launch(integral_constant<int, 4>{});
@@ -216,9 +216,11 @@ static int by_width(int64_t cols, Launch launch) {
   if (cols <= 1024) return launch(integral_constant<int, 32>{});
   if (cols <= 2048) return launch(integral_constant<int, 64>{});
   if (cols <= 4096) return launch(integral_constant<int, 128>{});
-  if (cols <= 8192) return launch(integral_constant<int, 256>{});
-  if (cols <= 16384) return launch(integral_constant<int, 512>{});
-  return launch(integral_constant<int, 1024>{});
+  if (MOST <= 256 || cols <= 8192) return launch(integral_constant<int, 256>{});
+  if constexpr (MOST > 256) {
+    if (cols <= 16384) return launch(integral_constant<int, 512>{});
+    return launch(integral_constant<int, 1024>{});
+  }
 }
 template <int THREADS>
 static dim3 row_grid(int64_t rows) {
@@ -241,7 +243,7 @@ static int pack_rows(const void* x, int64_t rows, int64_t cols, int64_t ldx, int
 template <int DTYPE, bool VEC>
 static int unpack_rows(const int8_t* codes, int64_t ldq, const float* scales, int64_t rows, int64_t cols, void* out, int64_t ldo, cudaStream_t st) {
   using T = typename Elem<DTYPE>::type;
-  return by_width(cols < kSpan ? cols : kSpan, [&](auto threads) {
+  return by_width<kSpan / 32>(cols < kSpan ? cols : kSpan, [&](auto threads) {
     constexpr int THREADS = threads;
     const int64_t spans = (cols + kSpan - 1) / kSpan, blocks = spans * row_grid<THREADS>(rows).x;
     if (blocks > NSML_Q8_MAX_ROWS) return (int)NSML_ERR_ARG;
