@@ -498,9 +498,10 @@ int nsml_q8_unpack(const int8_t* codes, int64_t ldq, const float* scales, int64_
  *                    be x or residual itself
  *   weight           cols elements of weight_dtype
  *   rstd             rows float32, may be NULL; the backward pass needs it
- *   eps              > 0;  cols <= NSML_Q8_MAX_NORM_COLS */
+ *   eps              > 0 as a float32 (it is used in float64);
+ *                    cols <= NSML_Q8_MAX_NORM_COLS */
 int nsml_q8_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t rows, int64_t cols, int dtype,
-                     const void* weight, int weight_dtype, float eps, void* h, int64_t ldh, int8_t* codes, int64_t ldq,
+                     const void* weight, int weight_dtype, double eps, void* h, int64_t ldh, int8_t* codes, int64_t ldq,
                      float* scales, float* rstd, void* stream);
 
 /* nsml_q8_rms_norm_backward -- its gradient (rounding to codes counts as the

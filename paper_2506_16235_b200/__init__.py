@@ -127,7 +127,7 @@ def _load() -> ctypes.CDLL:
         "nsml_q8_row_bytes": (i64, [i64]),
         "nsml_q8_pack": (ci, [vp, i64, i64, i64, ci, vp, i64, vp, vp]),
         "nsml_q8_unpack": (ci, [vp, i64, vp, i64, i64, vp, i64, ci, vp]),
-        "nsml_q8_rms_norm": (ci, [vp, i64, vp, i64, i64, i64, ci, vp, ci, ctypes.c_float, vp, i64, vp, i64, vp, vp, vp]),
+        "nsml_q8_rms_norm": (ci, [vp, i64, vp, i64, i64, i64, ci, vp, ci, dbl, vp, i64, vp, i64, vp, vp, vp]),
         "nsml_q8_rms_norm_backward_workspace_bytes": (sz, [i64]),
         "nsml_q8_rms_norm_backward": (ci, [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, ci, vp, ci, vp, i64, vp, ci,
                                            ci, vp, sz, vp]),

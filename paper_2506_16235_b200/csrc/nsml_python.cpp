@@ -194,7 +194,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {  // x, weight,
       !call.stream(&st))
     return nullptr;
   return result([&] {
-    return nsml_q8_rms_norm(x.ptr, x.ld, r.ptr, r.ld, x.rows, x.cols, x.dtype, w, wtype, (float)eps, h.ptr, h.ld, codes_of(q), q.ld, s, rstd, st);
+    return nsml_q8_rms_norm(x.ptr, x.ld, r.ptr, r.ld, x.rows, x.cols, x.dtype, w, wtype, eps, h.ptr, h.ld, codes_of(q), q.ld, s, rstd, st);
   });
 }
 

@@ -120,9 +120,8 @@ struct NormArgs {
   float* scales;
   float* rstd;           // may be null
   int64_t rows, ldx, ldr, ldh, ldq;
-  double inv_cols;
+  double inv_cols, eps;
   int cols;
-  float eps;
   bool weight_bf16;
 };
 
@@ -182,7 +181,7 @@ __global__ void __launch_bounds__(block_threads<THREADS>()) k_q8_norm(const Norm
     for (int j = 0; j < 8; ++j) sums[j & 3] = __fma_rn((double)y[i][j], (double)y[i][j], sums[j & 3]);
   }
   const double sum = row_sum<THREADS>((sums[0] + sums[1]) + (sums[2] + sums[3]), shared_sum);
-  const float rstd = (float)reciprocal_root(sum * a.inv_cols + (double)a.eps);
+  const float rstd = (float)reciprocal_root(sum * a.inv_cols + a.eps);
   if (lane == 0 && a.rstd != nullptr && row < a.rows) a.rstd[row] = rstd;
   float top = 0.0f;
 #pragma unroll
@@ -295,9 +294,9 @@ int nsml_q8_unpack(const int8_t* codes, int64_t ldq, const float* scales, int64_
 }
 
 int nsml_q8_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t rows, int64_t cols, int dtype,
-                     const void* weight, int weight_dtype, float eps, void* h, int64_t ldh, int8_t* codes, int64_t ldq,
+                     const void* weight, int weight_dtype, double eps, void* h, int64_t ldh, int8_t* codes, int64_t ldq,
                      float* scales, float* rstd, void* stream) {
-  if (!valid_type(dtype) || !valid_type(weight_dtype) || !valid_sizes(rows, cols, NSML_Q8_MAX_NORM_COLS) || !(eps > 0.0f) || !(eps <= 3.4e38f))
+  if (!valid_type(dtype) || !valid_type(weight_dtype) || !valid_sizes(rows, cols, NSML_Q8_MAX_NORM_COLS) || !((float)eps > 0.0f) || !(eps <= 3.4e38))
     return NSML_ERR_ARG;
   if (rows == 0) return NSML_OK;
   if (!valid_matrix(x, rows, cols, ldx, dtype) || !valid_codes(codes, rows, cols, ldq) || scales == nullptr || !aligned(scales, 4)) return NSML_ERR_ARG;
