@@ -125,12 +125,15 @@ struct NormArgs {
   bool weight_bf16;
 };
 
-// 1/sqrt(v): a Newton step in 64 bits on the float32 approximation (relative error 2^-22 -> 2^-43), where float32 holds v;
-// v > 0, or NaN.
+// 1/sqrt(v): two Newton steps in 64 bits on the float32 approximation (relative error 2^-22 -> 2^-43 -> a rounding or two of 64
+// bits), where float32 holds v; v > 0, or NaN.  With one step a root next to a border between two float32 may be rounded to the
+// wrong one.
 __device__ __forceinline__ double reciprocal_root(double v) {
   if (!(v > 1e-30 && v < 1e30)) return 1.0 / sqrt(v);
-  const double y = (double)rsqrtf((float)v);
-  return y * (1.5 - 0.5 * v * y * y);
+  double y = (double)rsqrtf((float)v);
+#pragma unroll
+  for (int step = 0; step < 2; ++step) y = __fma_rn(0.5 * y, __fma_rn(-(v * y), y, 1.0), y);
+  return y;
 }
 
 // h = rn(x + residual); rstd = 1/sqrt(sum h^2 / cols + eps): sum, quotient and root in 64 bits, rounded once, so that the
