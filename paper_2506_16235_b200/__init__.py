@@ -152,8 +152,25 @@ def _load() -> ctypes.CDLL:
     return lib
 
 
+class _NoNative:
+    """Stands in for the module of the 8-bit operators' calls where it cannot be loaded: nothing else needs it."""
+
+    def __init__(self, error):
+        self._error = error
+
+    def setup(self, *args):
+        pass
+
+    def __getattr__(self, name):
+        raise ImportError(f"{_build.NATIVE_PATH}, through which the 8-bit operators are called, cannot be loaded ({self._error}): "
+                          "build it with `python -m paper_2506_16235_b200.build` (needs g++ and, if the library is not built either, nvcc)")
+
+
 lib = _load()
-from . import _native  # noqa: E402  (linked to the library; built with it)
+try:
+    from . import _native  # (linked to the library; built with it)
+except ImportError as error:
+    _native = _NoNative(error)
 
 
 def nsml_strerror(status: int) -> str:

@@ -57,13 +57,17 @@ def _fingerprint() -> str:
     return h.hexdigest()
 
 
-def is_stale() -> bool:
-    """True if the library is missing or was built from other sources or flags
-    (content hash, so file times do not matter)."""
-    if not all(map(os.path.exists, (LIB_PATH, NATIVE_PATH, STAMP_PATH))):
+def _library_is_stale() -> bool:
+    if not (os.path.exists(LIB_PATH) and os.path.exists(STAMP_PATH)):
         return True
     with open(STAMP_PATH) as fh:
         return fh.read().strip() != _fingerprint()
+
+
+def is_stale() -> bool:
+    """True if the library or the module is missing or was built from other sources or flags
+    (content hash, so file times do not matter)."""
+    return _library_is_stale() or not os.path.exists(NATIVE_PATH)
 
 
 def _cxx() -> str:
@@ -90,8 +94,10 @@ def build_native(verbose: bool = False) -> None:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile the library if it is missing or older than its sources."""
-    if not force and not is_stale():
+    """Compile the library and the module if they are missing or older than their sources."""
+    if not force and not _library_is_stale():
+        if not os.path.exists(NATIVE_PATH):
+            build_native(verbose)
         return LIB_PATH
     cmd = [_nvcc()] + FLAGS + ["-I", INCLUDE, "-I", CSRC]
     if verbose:
