@@ -5,11 +5,11 @@
 //   kGradWeight   dw[n,k]  = sum_m dy[m,n] (a[m,k] sa[m])          the same, dy read across its rows
 //
 // Large products are bound by the tensor cores and, a few milliseconds into a loop, by the board's power (clocks of 1.2 to
-// 1.45 GHz).  8192 x 8192 x 2048 in a loop, one B200: kForward 100-107 us (2.6 to 2.7 10^15 operations per second; the library's
-// 8-bit product 99-117), the gradients 227-250 us (1.1 to 1.2; the library's bfloat16 product 180-210).  The gradients' distance
-// is the restoring: without it (timing only) 189-219.  Small ones are bound by latency: 4.1 us for 16 x 64 x 64 (gradients 5.1 and
-// 6.0), a third of a microsecond per step of the sum.  Large results of short sums are bound by storing them: 8192 x 16384 x 128 to
-// bfloat16 81 us (268 MB; with nothing stored 68).
+// 1.45 GHz).  8192 x 8192 x 2048 in a loop, one B200: kForward 100-111 us (2.5 to 2.7 10^15 operations per second; the library's
+// 8-bit product 99-117), the gradients 227-257 us (1.1 to 1.2; the library's bfloat16 product 180-210).  The gradients' distance
+// is the restoring of every code once per 256 rows of the result.  Small ones are bound by latency: 4.1 us for 16 x 64 x 64
+// (gradients 5.1 and 6.0), a third of a microsecond per step of the sum.  Large results of short sums are bound by the warps that
+// take them out: 8192 x 16384 x 128 to bfloat16 81 us (268 MB, 41 us of the memory's time).
 //
 // In the gradients the codes' scale belongs to the axis of the sum, so it cannot wait for the epilogue: eight warps restore
 // the codes to bfloat16 on their way from one shared-memory ring to another (exact for the scales that nsml_q8_pack makes).

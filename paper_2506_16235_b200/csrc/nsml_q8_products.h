@@ -7,7 +7,7 @@
 namespace nsml {
 namespace q8 {
 
-// Products of so many tokens or fewer have a kernel of their own.  n = 8192, k = 2048, one B200: 1 token 5.0 us (tensor cores
+// Products of so many tokens or fewer have a kernel of their own.  n = 8192, k = 2048 (from L2), one B200: 1 token 5.0 us (tensor cores
 // 8.7), 4 6.9 (9.4), 8 10.0 (9.4), 16 34 (9.4).
 constexpr int kMaxTokens = 4;
 

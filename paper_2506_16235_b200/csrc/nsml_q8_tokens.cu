@@ -1,7 +1,7 @@
 // Product of a few tokens with 8-bit weights: out[m, n] = (sum_k a[m,k] b[n,k]) sa[m] sb[n], m <= kMaxTokens.  The weights have to be read
 // once and nothing else counts, so no tensor cores: a warp takes kRows rows of the weights (so that the tokens' codes are
 // read once per kRows of them), its lanes 16 codes each, and multiplies with four-way integer products.  One token, n = 8192,
-// k = 2048 (17 MB): 5.0 us; n = k = 16384 46 us, 5.8 TB/s.
+// k = 2048 (17 MB): 5.0 us where L2 holds the weights, 7.5 from cold caches; n = k = 16384 (268 MB) 44 us, 6.1 TB/s.
 #include <type_traits>
 
 #include "nsml_launch.h"
