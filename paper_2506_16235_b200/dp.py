@@ -204,26 +204,30 @@ class NormLinear:
         if self.kept is None:
             raise RuntimeError("backward() without a forward() before it")
         rows, scales, rstd, (h_codes, h_scales) = self.kept
-        m, n = rows.shape[0], self.codes.shape[0]
+        shape, device, dtype = rows.shape, rows.device, dy.dtype
         # whatever a call below would refuse is refused here, before the first of them has written anything
-        if dy.dtype not in (torch.bfloat16, torch.float32):
-            raise TypeError(f"dy must be bfloat16 or float32, not {dy.dtype}")
-        for t, what, shape in ((dy, "dy", (m, n)), (dh, "dh", rows.shape)):
-            if t is None:
-                continue
-            if t.dtype is not dy.dtype:
-                raise TypeError(f"{what} must be {dy.dtype}, not {t.dtype}")
-            if tuple(t.shape) != tuple(shape) or t.device != self.codes.device:
-                raise ValueError(f"{what} must have shape {tuple(shape)} and be on {self.codes.device}")
-            if (t.shape[1] > 1 and t.stride(1) != 1) or (m > 1 and t.stride(0) < t.shape[1]):
-                raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
-        nsml, dnormed, dy = self.nsml, torch.empty(rows.shape, dtype=dy.dtype, device=rows.device), self._for_products(dy)
+        if dtype is not torch.bfloat16 and dtype is not torch.float32:
+            raise TypeError(f"dy must be bfloat16 or float32, not {dtype}")
+        self._check(dy, "dy", (shape[0], self.codes.shape[0]), device)
+        if dh is not None:
+            if dh.dtype is not dtype:
+                raise TypeError(f"dh must be {dtype}, not {dh.dtype}")
+            self._check(dh, "dh", shape, device)
+        nsml, dnormed, dy = self.nsml, rows.new_empty(shape, dtype=dtype), self._for_products(dy)
         nsml.nsml_q8_matmul_grad_weight(dy, rows, scales, dw=self.grad_weight, zero_first=zero_first, workspace=self.workspaces[1])
         nsml.nsml_q8_matmul_grad_input(dy, self.codes, self.scales, dx=dnormed, workspace=self.workspaces[2])
         nsml.nsml_q8_rms_norm_backward(dnormed, self.norm_weight, rstd, codes=h_codes, scales=h_scales, dh=dh, dx=dnormed,
                                        dweight=self.grad_norm_weight, zero_first=zero_first, workspace=self.norm_workspace)
         self.kept = None
         return dnormed
+
+    @staticmethod
+    def _check(t: torch.Tensor, what: str, shape, device) -> None:
+        if t.shape != shape or t.device != device:
+            raise ValueError(f"{what} must have shape {tuple(shape)} and be on {device}")
+        stride = t.stride()
+        if (shape[1] > 1 and stride[1] != 1) or (shape[0] > 1 and stride[0] < shape[1]):
+            raise ValueError(f"{what} must be a 2-D tensor with contiguous rows")
 
     @staticmethod
     def _for_products(dy: torch.Tensor) -> torch.Tensor:
